@@ -10,6 +10,8 @@
  *                  (the attention of the single verification forward pass)    (Section 3.2)
  *   cb_accept      take the target's greedy choice after every node and keep the longest verified
  *                  branch plus one more token                                 (Section 3.2)
+ * Beside it: cb_chunk_append and cb_chunk_attn bring prompts and single tokens into the paged cache and attend over it, cb_tree_rope
+ * makes the rotated queries and keys of a tree, cb_logprobs says how likely tokens were.
  *
  * Conventions
  *   - Every tensor pointer is a DEVICE pointer owned by the caller unless a parameter says "host".
@@ -330,6 +332,158 @@ typedef struct {
 } cb_kv_commit_args;
 
 cb_status cb_kv_commit(cb_ctx* ctx, const cb_kv_commit_args* args, void* stream);
+
+/*
+ * Queries, keys and values as a model's projection leaves them, for cb_chunk_append and cb_tree_rope (the paper leaves the model's own
+ * layers to the caller; these calls make what cb_chunk_attn and cb_tree_attn read).  Per head: an RMS norm of queries and keys, and the
+ * rotation by position in the same pass.  With x one head of a row, D = head_dim, R = rotary_dim:
+ *   y = x / sqrt(mean(x^2) + eps) * w                       (no norm where w is NULL)
+ *   (y_a, y_b) -> (y_a c_i - y_b s_i, y_b c_i + y_a s_i)     for i < R / 2, with (a, b) = (i, i + R / 2), or (2i, 2i + 1) if interleaved;
+ *                                                            c_i = rope[pos][i], s_i = rope[pos][R / 2 + i]; elements from R on stay
+ * in fp32, rounded to bf16 once at the end.  Values are copied.
+ *   q, k, v     bf16; head h of row r starts q_stride * r + h * D elements from the base (k, v alike), so that the three may be parts of
+ *               one projected row
+ *   q_norm, k_norm  bf16 [D] or NULL
+ *   rope        float [rope_len, R], or NULL for no rotation
+ * Base pointers are 16-byte aligned, strides multiples of 8, R a multiple of 16 and at most D, eps >= 0.
+ */
+typedef struct {
+    const void* q;
+    const void* k;
+    const void* v;
+    int64_t q_stride, k_stride, v_stride;
+    const void* q_norm;
+    const void* k_norm;
+    float eps;
+    const float* rope;
+    int32_t rope_len, rotary_dim, interleaved;
+} cb_qkv_rows;
+
+/*
+ * Appends a chunk of new tokens per sequence (a prompt, a part of one, or a single token) to the paged cache and makes their queries.
+ * The chunks lie one behind the other: sequence b's are rows q_start[b] .. q_start[b + 1), and row q_start[b] + i is the token at
+ * position ctx_len[b] + i.
+ *   q_start     int32 [batch + 1]               non-decreasing, <= n_rows; a sequence without new tokens has an empty range
+ *   ctx_len     int32 [batch]                   tokens cached before this chunk; only read, so that every layer of a model can be given
+ *                                               the same lengths (the caller adds the chunk lengths after the last one)
+ *   block_table int32 [batch, max_pages]        must already name pages for the new positions
+ *   q_out       bf16 [n_rows, Hq, D]            may be q itself where q_stride = Hq * D
+ *   k_pool, v_pool  bf16 [num_pages, P, Hkv, D] written at the new positions only
+ * Rows that belong to no sequence (before q_start[0], from q_start[batch] on) are left as they were.  A sequence whose pages cannot
+ * hold the new tokens is left alone (no row of it is written) and CB_ERR_KV_FULL is recorded in the device status; a row whose position
+ * the rope table does not have, or whose page lies outside the pool, is left alone and CB_ERR_INVALID_ARG recorded.
+ */
+typedef struct {
+    cb_qkv_rows rows;
+    const int32_t* q_start;
+    const int32_t* ctx_len;
+    const int32_t* block_table;
+    int32_t n_rows;
+    int32_t max_pages;
+    int32_t num_pages;
+    void* q_out;
+    void* k_pool;
+    void* v_pool;
+} cb_chunk_append_args;
+
+cb_status cb_chunk_append(cb_ctx* ctx, const cb_chunk_append_args* args, void* stream);
+
+/*
+ * The same for the nodes of a draft tree before their verification pass: row b * T + i is node i of sequence b, at position
+ * ctx_len[b] + tree_depth[b][i] (T = max_nodes; the root is the first token that is not cached).
+ *   tree_depth int32 [batch, T], n_nodes int32 [batch]   as written by cb_draft_tree;  ctx_len int32 [batch]
+ *   q_out bf16 [batch, T, Hq, D]; k_out, v_out bf16 [batch, T, Hkv, D]   the tensors that cb_tree_attn and cb_kv_commit read; each may be
+ *              its input where that is laid out the same way
+ * Rows from n_nodes on are written as zero (cb_tree_attn wants them finite).  A node whose position the rope table does not have is
+ * written as zero and CB_ERR_INVALID_ARG recorded.
+ */
+typedef struct {
+    cb_qkv_rows rows;
+    const int32_t* tree_depth;
+    const int32_t* n_nodes;
+    const int32_t* ctx_len;
+    void* q_out;
+    void* k_out;
+    void* v_out;
+} cb_tree_rope_args;
+
+cb_status cb_tree_rope(cb_ctx* ctx, const cb_tree_rope_args* args, void* stream);
+
+/*
+ * Causal attention of each sequence's chunk of new tokens over its paged cache, the chunk's own keys and values included
+ * (cb_chunk_append has put them there): row q_start[b] + i attends to cached positions 0 .. ctx_len[b] + i.
+ *   q            bf16 [n_rows, Hq, D]
+ *   k_pool, v_pool, block_table   as in cb_tree_attn;  q_start, ctx_len   as in cb_chunk_append
+ *   out          bf16 [n_rows, Hq, D]
+ *   lse          float [n_rows, Hq] or NULL     natural-log sum of exponentials per row
+ *   max_chunk    host upper bound on every chunk length (0 = n_rows); with chunks of few tokens it decides how the work is split
+ *   max_ctx      host upper bound on every ctx_len + chunk length (0 = max_pages * P)
+ *   scale        softmax scale; 0 selects 1/sqrt(D)
+ * fp32 accumulation and softmax, output rounded to bf16; equal calls give equal bits, as in cb_tree_attn.
+ * Rows that belong to no sequence are left as they were.  A sequence whose cached and new tokens exceed max_pages * P, or max_ctx, is
+ * left alone and CB_ERR_KV_FULL recorded; one whose range is not inside [0, n_rows], or longer than max_chunk, or whose ctx_len is
+ * negative, is left alone and CB_ERR_INVALID_ARG recorded.  A page outside the pool reads as zeros.
+ * Slots of the last, partly filled page beyond the sequence's tokens may hold anything; the tokens' own keys and values must be finite.
+ * out must not be q.  Base pointers are 16-byte aligned.
+ */
+typedef struct {
+    const void* q;
+    const void* k_pool;
+    const void* v_pool;
+    const int32_t* block_table;
+    const int32_t* q_start;
+    const int32_t* ctx_len;
+    void* out;
+    float* lse;
+    int32_t n_rows;
+    int32_t max_pages;
+    int32_t num_pages;
+    int32_t max_chunk;
+    int32_t max_ctx;
+    float scale;
+} cb_chunk_attn_args;
+
+cb_status cb_chunk_attn(cb_ctx* ctx, const cb_chunk_attn_args* args, void* stream);
+
+/*
+ * How likely tokens were: for each of n_out rows of logits x over vocab tokens, with Z = sum_v exp(x_v),
+ *   logprobs[i]  = x_t - log Z              t = tokens[i]
+ *   entropy[i]   = log Z - sum_v p_v x_v    p = exp(x) / Z
+ *   top_ids[i], top_logprobs[i]             the top_k largest x_v (equal ones by rising id) and their x_v - log Z, largest first
+ * fp32 throughout.  Logits are finite or -inf (a forbidden token: probability 0, no part of the entropy); a row with a NaN or +inf, or
+ * without a finite logit, gives NaN.
+ *   logits        [n_rows, vocab] of logits_dtype, rows logits_row_stride elements apart
+ *   rows          int32 [n_out]: the row of logits of each output, or NULL for row i (n_out <= n_rows)
+ *   tokens        int32 [n_out], or NULL: logprobs is then not written
+ *   logprobs, entropy  float [n_out], each or NULL
+ *   top_ids       int32 [n_out, top_k], top_logprobs float [n_out, top_k]; top_k 0..CB_MAX_TOP; with fewer than top_k tokens in the vocabulary the
+ *                 rest is -1 and -inf
+ * An output with a negative token, or a negative row, is padding: its row is not read, logprobs and entropy are 0, top_ids -1,
+ * top_logprobs 0.  A token >= vocab or a row >= n_rows is treated the same way and CB_ERR_INVALID_ARG recorded.
+ *
+ * cb_accept_logprobs: the same for the tokens that cb_accept emitted, from the logits it was given.  Output (b, j) is for
+ * out_tokens[b][j], whose row is that of node 0 for j = 0 and of accept_nodes[b][j - 1] behind it; the places behind the bonus token
+ * (out_tokens -1) are padding.  Outputs have leading dimensions [batch, max_depth + 1]; logits are [batch, max_nodes, vocab].
+ */
+enum { CB_MAX_TOP = 32 };
+typedef struct {
+    const void* logits;
+    int32_t logits_dtype;
+    int64_t logits_row_stride;
+    int32_t n_rows;
+    int32_t n_out;
+    const int32_t* rows;
+    const int32_t* tokens;
+    int32_t top_k;
+    float* logprobs;
+    float* entropy;
+    int32_t* top_ids;
+    float* top_logprobs;
+} cb_logprobs_args;
+
+cb_status cb_logprobs(cb_ctx* ctx, const cb_logprobs_args* args, void* stream);
+/* args->n_rows, n_out, rows and tokens are not read. */
+cb_status cb_accept_logprobs(cb_ctx* ctx, const int32_t* accept_nodes, const int32_t* out_tokens, const cb_logprobs_args* args, void* stream);
 
 /*
  * Frozen table (Section 3.3): a second, read-only table built offline from the most frequent leader-follower pairs of a

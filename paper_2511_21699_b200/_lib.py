@@ -16,6 +16,7 @@ CB_ERR_KV_FULL = 8
 CB_ERR_INVALID_ARG, CB_ERR_CANARY = 1, 9
 CB_GUARD_BYTES = 256
 CB_STATIC_MAX_BATCH, CB_STATIC_MAX_ROWS = 1024, 8192
+CB_MAX_TOP = 32
 CB_NUM_COUNTERS = 8
 COUNTER_NAMES = ["inserts", "leader_evictions", "follower_evictions", "queries", "query_hits", "max_probe", "frozen_queries",
                  "frozen_hits"]
@@ -24,7 +25,8 @@ EXPORTS = ["cb_workspace_bytes", "cb_create", "cb_destroy", "cb_reset", "cb_upda
            "cb_tree_attn", "cb_accept", "cb_table_dump", "cb_table_load", "cb_poll_status", "cb_launch_count",
            "cb_status_str", "cb_accept_static", "cb_kv_commit", "cb_frozen_bytes", "cb_frozen_load", "cb_frozen_dump",
            "cb_frozen_attach", "cb_frozen_build_bytes", "cb_frozen_build", "cb_tree_add_branches", "cb_update_bulk", "cb_debug_build",
-           "cb_bulk_scratch_bytes", "cb_bulk_scratch_attach", "cb_accept_update_draft_tree"]
+           "cb_bulk_scratch_bytes", "cb_bulk_scratch_attach", "cb_accept_update_draft_tree", "cb_chunk_append", "cb_tree_rope",
+           "cb_chunk_attn", "cb_logprobs", "cb_accept_logprobs"]
 
 
 class CbConfigC(C.Structure):
@@ -54,6 +56,32 @@ class CbAttnArgsC(C.Structure):
                [("max_pages", C.c_int32), ("num_pages", C.c_int32), ("max_ctx", C.c_int32), ("scale", C.c_float)]
 
 
+class CbQkvRowsC(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("q", "k", "v")] + [(n, C.c_int64) for n in ("q_stride", "k_stride", "v_stride")] + \
+               [("q_norm", C.c_void_p), ("k_norm", C.c_void_p), ("eps", C.c_float), ("rope", C.c_void_p)] + \
+               [(n, C.c_int32) for n in ("rope_len", "rotary_dim", "interleaved")]
+
+
+class CbChunkAppendArgsC(C.Structure):
+    _fields_ = [("rows", CbQkvRowsC)] + [(n, C.c_void_p) for n in ("q_start", "ctx_len", "block_table")] + \
+               [(n, C.c_int32) for n in ("n_rows", "max_pages", "num_pages")] + [(n, C.c_void_p) for n in ("q_out", "k_pool", "v_pool")]
+
+
+class CbTreeRopeArgsC(C.Structure):
+    _fields_ = [("rows", CbQkvRowsC)] + [(n, C.c_void_p) for n in ("tree_depth", "n_nodes", "ctx_len", "q_out", "k_out", "v_out")]
+
+
+class CbChunkAttnArgsC(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("q", "k_pool", "v_pool", "block_table", "q_start", "ctx_len", "out", "lse")] + \
+               [(n, C.c_int32) for n in ("n_rows", "max_pages", "num_pages", "max_chunk", "max_ctx")] + [("scale", C.c_float)]
+
+
+class CbLogprobsArgsC(C.Structure):
+    _fields_ = [("logits", C.c_void_p), ("logits_dtype", C.c_int32), ("logits_row_stride", C.c_int64), ("n_rows", C.c_int32), ("n_out", C.c_int32),
+                ("rows", C.c_void_p), ("tokens", C.c_void_p), ("top_k", C.c_int32)] + \
+               [(n, C.c_void_p) for n in ("logprobs", "entropy", "top_ids", "top_logprobs")]
+
+
 _lib = None
 
 
@@ -81,6 +109,11 @@ def load():
     L.cb_tree_attn.argtypes = [vp, C.POINTER(CbAttnArgsC), vp]
     L.cb_accept_update_draft_tree.argtypes = [vp, C.POINTER(CbAcceptDraftArgsC), vp]
     L.cb_kv_commit.argtypes = [vp, C.POINTER(CbKvCommitArgsC), vp]
+    L.cb_chunk_append.argtypes = [vp, C.POINTER(CbChunkAppendArgsC), vp]
+    L.cb_tree_rope.argtypes = [vp, C.POINTER(CbTreeRopeArgsC), vp]
+    L.cb_chunk_attn.argtypes = [vp, C.POINTER(CbChunkAttnArgsC), vp]
+    L.cb_logprobs.argtypes = [vp, C.POINTER(CbLogprobsArgsC), vp]
+    L.cb_accept_logprobs.argtypes = [vp, vp, vp, C.POINTER(CbLogprobsArgsC), vp]
     L.cb_accept.argtypes = [vp, vp, vp, vp, vp, vp, i32, i64, vp, vp, vp, vp, vp, vp]
     L.cb_accept_static.argtypes = [i32, i32, i32, i32, vp, vp, vp, vp, vp, i32, i64, vp, vp, vp, vp, vp]
     L.cb_table_dump.argtypes = [vp, i32, C.POINTER(i32), vp, vp, vp]

@@ -37,7 +37,8 @@ def _stream(stream):
 
 
 _BOUND = ("cb_reset", "cb_update", "cb_update_bulk", "cb_draft_tree", "cb_update_draft_tree", "cb_tree_attn", "cb_accept",
-          "cb_accept_update_draft_tree", "cb_kv_commit", "cb_status_str")
+          "cb_accept_update_draft_tree", "cb_kv_commit", "cb_chunk_append", "cb_chunk_attn", "cb_tree_rope", "cb_logprobs", "cb_accept_logprobs",
+          "cb_status_str")
 _host_module = None
 try:                                     # loaded with the package (some 40 ms), not by the first context; not there yet while it is built
     from . import _binding
@@ -168,6 +169,8 @@ class Cacheback:
             _check(self.lib.cb_create(C.byref(self.cfg), base, nbytes.value, C.byref(h)), "cb_create")
         self._h = h
         self.W = (max_nodes + 31) // 32
+        index = self.device.index if self.device.index is not None else torch.cuda.current_device()
+        self._shape = (index, batch, max_nodes, n_q_heads, n_kv_heads, head_dim, page_size, max_depth, vocab)
 
     @classmethod
     def from_config(cls, cfg, flags=0, device="cuda:0", batch=None):
@@ -266,6 +269,64 @@ class Cacheback:
         res = res if res is not None else self.alloc_accept()
         next_tree = next_tree if next_tree is not None else tree
         self._host.accept_update_draft_tree(self._h, tree, logits, tokens, seq_len, next_tree, res, stream)
+        return res
+
+    # ---- beside the step: prompts and single tokens into the cache, likelihoods ------------------------
+    def cb_chunk_append(self, q, k, v, q_start, ctx_len, k_pool, v_pool, block_table, rope=None, q_norm=None, k_norm=None, eps=1e-6,
+                        interleaved=False, q_out=None, stream=None):
+        """The new tokens of all sequences, one chunk behind the other (sequence b's are rows q_start[b]..q_start[b + 1]): per-head norm and
+        rotation of q and k, k and v into the pages behind the ctx_len[b] cached tokens.  q, k, v [rows, heads, head_dim], each row
+        contiguous (they may be parts of one projection).  Returns the queries [rows, n_q_heads, head_dim]; ctx_len is not advanced."""
+        if q_out is None:
+            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        self._host.chunk_append(self._h, self._shape, q, k, v, q_norm, k_norm, eps, rope, interleaved, q_start, ctx_len, k_pool, v_pool, block_table,
+                                q_out, stream)
+        return q_out
+
+    def cb_chunk_attn(self, q, k_pool, v_pool, block_table, q_start, ctx_len, out=None, lse=None, max_chunk=0, max_ctx=0, scale=0.0, stream=None):
+        """Causal attention of each sequence's new tokens over its cached ones and themselves, after cb_chunk_append has put their
+        keys and values into the pages.  max_chunk, max_ctx: host upper bounds on the new tokens of a sequence and on its cached and
+        new tokens together (0: not known)."""
+        if out is None:
+            out = torch.empty_like(q)
+        self._host.chunk_attn(self._h, self._shape, q, k_pool, v_pool, block_table, q_start, ctx_len, out, lse, max_chunk, max_ctx, scale, stream)
+        return out
+
+    def cb_tree_rope(self, q, k, v, tree, ctx_len, rope=None, q_norm=None, k_norm=None, eps=1e-6, interleaved=False, q_out=None, k_out=None,
+                     v_out=None, stream=None):
+        """The norm and rotation of cb_chunk_append for the nodes of a draft tree (row b * max_nodes + i is node i of sequence b, at
+        position ctx_len[b] + depth): the q, k_tree and v_tree that cb_tree_attn takes, rows behind n_nodes zero."""
+        c = self.cfg
+        new = lambda heads: torch.empty(c.batch, c.max_nodes, heads, c.head_dim, dtype=torch.bfloat16, device=self.device)
+        q_out = q_out if q_out is not None else new(c.n_q_heads)
+        k_out = k_out if k_out is not None else new(c.n_kv_heads)
+        v_out = v_out if v_out is not None else new(c.n_kv_heads)
+        self._host.tree_rope(self._h, self._shape, q, k, v, q_norm, k_norm, eps, rope, interleaved, tree, ctx_len, q_out, k_out, v_out, stream)
+        return q_out, k_out, v_out
+
+    def _alloc_logprobs(self, lead, top_k):
+        f32, i32 = dict(dtype=torch.float32, device=self.device), dict(dtype=torch.int32, device=self.device)
+        res = dict(logprobs=torch.empty(lead, **f32), entropy=torch.empty(lead, **f32))
+        if top_k > 0:
+            res.update(top_ids=torch.empty(*lead, top_k, **i32), top_logprobs=torch.empty(*lead, top_k, **f32))
+        return res
+
+    def cb_logprobs(self, logits, tokens, rows=None, top_k=0, res=None, stream=None):
+        """Log probability of tokens[i] under row i of logits [n, vocab] (row rows[i] where given), the row's entropy and its top_k best tokens with
+        their log probabilities (equal ones by rising id).  Negative tokens or rows are padding.  tokens None: no log probability
+        (logprobs is not written)."""
+        if res is None:
+            n = rows if rows is not None else (tokens if tokens is not None else logits)
+            res = self._alloc_logprobs((int(n.shape[0]),), top_k)
+        self._host.logprobs(self._h, self._shape, logits, tokens, rows, top_k, res, stream)
+        return res
+
+    def cb_accept_logprobs(self, logits, accepted, top_k=0, res=None, stream=None):
+        """The same for the tokens that cb_accept emitted (`accepted`: its result), from the logits that it was given: outputs
+        [batch, max_depth + 1], padding behind the last emitted token."""
+        if res is None:
+            res = self._alloc_logprobs((self.cfg.batch, self.cfg.max_depth + 1), top_k)
+        self._host.accept_logprobs(self._h, self._shape, logits, accepted, top_k, res, stream)
         return res
 
     # ---- helpers ------------------------------------------------------------------------------------

@@ -9,7 +9,9 @@
 #include <Python.h>
 
 #include <algorithm>
+#include <initializer_list>
 
+#include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -31,6 +33,11 @@ struct Library {
     decltype(&cb_accept) accept;
     decltype(&cb_accept_update_draft_tree) accept_update_draft_tree;
     decltype(&cb_kv_commit) kv_commit;
+    decltype(&cb_chunk_append) chunk_append;
+    decltype(&cb_chunk_attn) chunk_attn;
+    decltype(&cb_tree_rope) tree_rope;
+    decltype(&cb_logprobs) logprobs;
+    decltype(&cb_accept_logprobs) accept_logprobs;
     decltype(&cb_status_str) status_str;
 } g_lib;
 
@@ -253,6 +260,221 @@ void do_kv_commit(PyObject* const* a) {
     call("cb_kv_commit", [&] { return g_lib.kv_commit(c, &x, st); });
 }
 
+// ---- the operators beside the step.  Their shapes are checked against the context's, which api.py hands over as a tuple.
+struct Shape { int64_t device, B, T, Hq, Hkv, D, P, Dmax, V; };
+Shape shape_of(PyObject* o) {
+    int64_t v[9];
+    if (!PyTuple_Check(o) || PyTuple_GET_SIZE(o) != 9) { PyErr_SetString(PyExc_TypeError, "expected the context's shape"); throw Refused(); }
+    for (int k = 0; k < 9; ++k) v[k] = long_of(PyTuple_GET_ITEM(o, k));
+    return {v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7], v[8]};
+}
+[[noreturn]] void refuse_shape(const char* name, const char* want) {
+    PyErr_Format(g_error, "%s must be %s", name, want);
+    throw Refused();
+}
+// A CUDA tensor on the context's device, of the given type and shape (-1: any size).  Contiguous unless `rows` is set: then its first
+// dimension may have any stride.
+struct Arg { const at::Tensor* t; void* p; };
+Arg arg(const Shape& s, PyObject* o, const char* name, at::ScalarType type, std::initializer_list<int64_t> want, const char* text, bool rows = false) {
+    const at::Tensor& t = tensor_of(o);
+    if (!t.is_cuda()) refuse("expected a contiguous CUDA tensor");
+    if (t.get_device() != s.device) refuse_shape(name, "on the context's device");
+    if (t.scalar_type() != type) {
+        PyObject* d = PyObject_GetAttrString(o, "dtype");
+        if (d) { PyErr_Format(g_error, "%s: expected dtype %s, got %S", name, type_name(type), d); Py_DECREF(d); }
+        throw Refused();
+    }
+    bool ok = t.dim() == (int64_t)want.size();
+    int64_t k = 0;
+    for (int64_t w : want) { ok = ok && (w < 0 || t.size(k) == w); ++k; }
+    if (!ok) refuse_shape(name, text);
+    if (!rows && !t.is_contiguous()) refuse("expected a contiguous CUDA tensor");
+    return {&t, t.data_ptr()};
+}
+template <typename T>
+T* opt(const Shape& s, PyObject* o, const char* name, at::ScalarType type, std::initializer_list<int64_t> want, const char* text) {
+    return o == Py_None ? nullptr : static_cast<T*>(arg(s, o, name, type, want, text).p);
+}
+// The stream to launch on: the one given, or the current one of the context's device, which is the current device for the call.
+struct OnDevice {
+    c10::cuda::CUDAGuard guard;
+    void* stream;
+    OnDevice(const Shape& s, PyObject* o) : guard((c10::DeviceIndex)s.device) {
+        stream = o == Py_None ? c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)s.device).stream() : stream_of(o);
+    }
+};
+int32_t int_of(PyObject* o, const char* name) {
+    const int64_t v = long_of(o);
+    if (v < INT32_MIN || v > INT32_MAX) refuse_shape(name, "a 32-bit number");
+    return (int32_t)v;
+}
+float float_of(PyObject* o) {
+    const double v = PyFloat_AsDouble(o);
+    if (v == -1.0 && PyErr_Occurred()) throw Refused();
+    return (float)v;
+}
+// q, k, v: [rows, heads, head_dim] with the heads of a row side by side, any stride from row to row
+const void* heads_of(const Shape& s, PyObject* o, const char* name, int64_t rows, int64_t heads, int64_t* stride) {
+    const Arg a = arg(s, o, name, at::kBFloat16, {rows, heads, s.D}, "[rows, heads, head_dim] of the context's heads, with a row per token", true);
+    const at::Tensor& t = *a.t;
+    if (t.numel() > 0 && (t.stride(2) != 1 || (heads > 1 && t.stride(1) != s.D))) refuse_shape(name, "contiguous within a row");
+    *stride = t.size(0) > 1 ? t.stride(0) : heads * s.D;
+    return a.p;
+}
+int64_t rows_of(PyObject* o) {
+    const at::Tensor& t = tensor_of(o);
+    if (t.dim() != 3 || t.size(0) > INT32_MAX) refuse_shape("q", "[rows, heads, head_dim]");
+    return t.size(0);
+}
+// q, k, v, q_norm, k_norm, eps, rope, interleaved
+cb_qkv_rows qkv_of(const Shape& s, PyObject* const* a, int64_t n) {
+    const auto bf = at::kBFloat16;
+    cb_qkv_rows r = {};
+    r.q = heads_of(s, a[0], "q", n, s.Hq, &r.q_stride);
+    r.k = heads_of(s, a[1], "k", n, s.Hkv, &r.k_stride);
+    r.v = heads_of(s, a[2], "v", n, s.Hkv, &r.v_stride);
+    r.q_norm = opt<void>(s, a[3], "q_norm", bf, {s.D}, "[head_dim]");
+    r.k_norm = opt<void>(s, a[4], "k_norm", bf, {s.D}, "[head_dim]");
+    r.eps = float_of(a[5]);
+    if (a[6] != Py_None) {
+        const Arg t = arg(s, a[6], "rope", at::kFloat, {-1, -1}, "[positions, rotary_dim]");
+        r.rope = static_cast<const float*>(t.p);
+        r.rope_len = (int32_t)std::min<int64_t>(t.t->size(0), INT32_MAX);
+        r.rotary_dim = (int32_t)std::min<int64_t>(t.t->size(1), INT32_MAX);
+        if (!r.rope) refuse_shape("rope", "[positions, rotary_dim] with at least one position");
+    }
+    const int inter = PyObject_IsTrue(a[7]);
+    if (inter < 0) throw Refused();
+    r.interleaved = inter;
+    return r;
+}
+struct Cache { void *k, *v; int32_t* table; int32_t max_pages, num_pages; };
+Cache cache_of(const Shape& s, PyObject* k, PyObject* v, PyObject* table) {
+    const auto bf = at::kBFloat16;
+    const Arg kp = arg(s, k, "k_pool", bf, {-1, s.P, s.Hkv, s.D}, "[pages, page_size, n_kv_heads, head_dim]");
+    const Arg vp = arg(s, v, "v_pool", bf, {kp.t->size(0), s.P, s.Hkv, s.D}, "of k_pool's shape");
+    const Arg bt = arg(s, table, "block_table", at::kInt, {s.B, -1}, "[batch, pages]");
+    if (kp.t->size(0) > INT32_MAX || bt.t->size(1) > INT32_MAX) refuse_shape("k_pool", "of less than 2^31 pages");
+    return {kp.p, vp.p, static_cast<int32_t*>(bt.p), (int32_t)bt.t->size(1), (int32_t)kp.t->size(0)};
+}
+// handle, shape, q, k, v, q_norm, k_norm, eps, rope, interleaved, q_start, ctx_len, k_pool, v_pool, block_table, q_out, stream
+void do_chunk_append(PyObject* const* a) {
+    cb_ctx* c = ctx_of(a[0]);
+    const Shape s = shape_of(a[1]);
+    cb_chunk_append_args x = {};
+    const int64_t n = rows_of(a[2]);
+    x.rows = qkv_of(s, a + 2, n);
+    x.n_rows = (int32_t)n;
+    x.q_start = static_cast<int32_t*>(arg(s, a[10], "q_start", at::kInt, {s.B + 1}, "[batch + 1]").p);
+    x.ctx_len = static_cast<int32_t*>(arg(s, a[11], "ctx_len", at::kInt, {s.B}, "[batch]").p);
+    const Cache k = cache_of(s, a[12], a[13], a[14]);
+    x.k_pool = k.k; x.v_pool = k.v; x.block_table = k.table; x.max_pages = k.max_pages; x.num_pages = k.num_pages;
+    x.q_out = arg(s, a[15], "q_out", at::kBFloat16, {n, s.Hq, s.D}, "[rows, n_q_heads, head_dim]").p;
+    if (n == 0) return;                                       // tensors without elements have no memory
+    const OnDevice on(s, a[16]);
+    call("cb_chunk_append", [&] { return g_lib.chunk_append(c, &x, on.stream); });
+}
+// handle, shape, q, k, v, q_norm, k_norm, eps, rope, interleaved, tree, ctx_len, q_out, k_out, v_out, stream
+void do_tree_rope(PyObject* const* a) {
+    cb_ctx* c = ctx_of(a[0]);
+    const Shape s = shape_of(a[1]);
+    cb_tree_rope_args x = {};
+    x.rows = qkv_of(s, a + 2, s.B * s.T);
+    {
+        Ref depth(PyObject_GetItem(a[10], s_depth)), n(PyObject_GetItem(a[10], s_n_nodes));
+        x.tree_depth = static_cast<int32_t*>(arg(s, depth.o, "depth", at::kInt, {s.B, s.T}, "[batch, max_nodes]").p);
+        x.n_nodes = static_cast<int32_t*>(arg(s, n.o, "n_nodes", at::kInt, {s.B}, "[batch]").p);
+    }
+    x.ctx_len = static_cast<int32_t*>(arg(s, a[11], "ctx_len", at::kInt, {s.B}, "[batch]").p);
+    x.q_out = arg(s, a[12], "q_out", at::kBFloat16, {s.B, s.T, s.Hq, s.D}, "[batch, max_nodes, n_q_heads, head_dim]").p;
+    x.k_out = arg(s, a[13], "k_out", at::kBFloat16, {s.B, s.T, s.Hkv, s.D}, "[batch, max_nodes, n_kv_heads, head_dim]").p;
+    x.v_out = arg(s, a[14], "v_out", at::kBFloat16, {s.B, s.T, s.Hkv, s.D}, "[batch, max_nodes, n_kv_heads, head_dim]").p;
+    const OnDevice on(s, a[15]);
+    call("cb_tree_rope", [&] { return g_lib.tree_rope(c, &x, on.stream); });
+}
+// handle, shape, q, k_pool, v_pool, block_table, q_start, ctx_len, out, lse, max_chunk, max_ctx, scale, stream
+void do_chunk_attn(PyObject* const* a) {
+    cb_ctx* c = ctx_of(a[0]);
+    const Shape s = shape_of(a[1]);
+    cb_chunk_attn_args x = {};
+    const int64_t n = rows_of(a[2]);
+    const auto bf = at::kBFloat16;
+    x.q = arg(s, a[2], "q", bf, {n, s.Hq, s.D}, "[rows, n_q_heads, head_dim]").p;
+    x.n_rows = (int32_t)n;
+    const Cache k = cache_of(s, a[3], a[4], a[5]);
+    x.k_pool = k.k; x.v_pool = k.v; x.block_table = k.table; x.max_pages = k.max_pages; x.num_pages = k.num_pages;
+    x.q_start = static_cast<int32_t*>(arg(s, a[6], "q_start", at::kInt, {s.B + 1}, "[batch + 1]").p);
+    x.ctx_len = static_cast<int32_t*>(arg(s, a[7], "ctx_len", at::kInt, {s.B}, "[batch]").p);
+    x.out = arg(s, a[8], "out", bf, {n, s.Hq, s.D}, "of q's shape").p;
+    x.lse = opt<float>(s, a[9], "lse", at::kFloat, {n, s.Hq}, "[rows, n_q_heads]");
+    x.max_chunk = int_of(a[10], "max_chunk");
+    x.max_ctx = int_of(a[11], "max_ctx");
+    x.scale = float_of(a[12]);
+    if (n == 0) return;
+    const OnDevice on(s, a[13]);
+    call("cb_chunk_attn", [&] { return g_lib.chunk_attn(c, &x, on.stream); });
+}
+// The outputs of log probabilities: a dictionary with logprobs and entropy, and the alternatives where there are any.
+void likely_of(const Shape& s, PyObject* res, PyObject* top, bool accept, int64_t n, cb_logprobs_args* x) {
+    x->top_k = int_of(top, "top_k");
+    if (x->top_k < 0 || x->top_k > CB_MAX_TOP) refuse_shape("top_k", "between 0 and 32");
+    const char* text = accept ? "[batch, max_depth + 1], alternatives [batch, max_depth + 1, top_k]" : "[outputs], alternatives [outputs, top_k]";
+    auto get = [&](const char* name, at::ScalarType t, bool many) -> void* {
+        Ref r(PyMapping_GetItemString(res, name));
+        if (accept) return many ? arg(s, r.o, name, t, {s.B, s.Dmax + 1, x->top_k}, text).p : arg(s, r.o, name, t, {s.B, s.Dmax + 1}, text).p;
+        return many ? arg(s, r.o, name, t, {n, x->top_k}, text).p : arg(s, r.o, name, t, {n}, text).p;
+    };
+    x->logprobs = static_cast<float*>(get("logprobs", at::kFloat, false));
+    x->entropy = static_cast<float*>(get("entropy", at::kFloat, false));
+    if (x->top_k == 0) return;
+    x->top_ids = static_cast<int32_t*>(get("top_ids", at::kInt, true));
+    x->top_logprobs = static_cast<float*>(get("top_logprobs", at::kFloat, true));
+}
+int32_t logits_dtype_of(const Shape& s, const at::Tensor& t) {
+    if (t.scalar_type() != at::kFloat && t.scalar_type() != at::kBFloat16) refuse("logits must be float32 or bfloat16");
+    if (!t.is_cuda() || t.get_device() != s.device) refuse_shape("logits", "on the context's device");
+    return t.scalar_type() == at::kFloat ? CB_DTYPE_F32 : CB_DTYPE_BF16;
+}
+// handle, shape, logits, tokens, rows, top_k, res, stream
+void do_logprobs(PyObject* const* a) {
+    cb_ctx* c = ctx_of(a[0]);
+    const Shape s = shape_of(a[1]);
+    cb_logprobs_args x = {};
+    const at::Tensor& t = tensor_of(a[2]);
+    x.logits_dtype = logits_dtype_of(s, t);
+    if (t.dim() != 2 || t.size(1) != s.V || t.size(0) > INT32_MAX || (t.numel() > 0 && s.V > 1 && t.stride(1) != 1))
+        refuse_shape("logits", "[rows, vocab], contiguous within a row");
+    x.n_rows = (int32_t)t.size(0);
+    x.logits = t.data_ptr();
+    x.logits_row_stride = t.size(0) > 1 ? t.stride(0) : s.V;
+    const int64_t n = a[4] != Py_None ? tensor_of(a[4]).numel() : (a[3] != Py_None ? tensor_of(a[3]).numel() : t.size(0));
+    if (n > INT32_MAX || (a[4] == Py_None && n > t.size(0))) refuse_shape("tokens", "at most one per row of logits");
+    x.n_out = (int32_t)n;
+    x.tokens = opt<int32_t>(s, a[3], "tokens", at::kInt, {n}, "[outputs]");
+    x.rows = opt<int32_t>(s, a[4], "rows", at::kInt, {n}, "[outputs]");
+    likely_of(s, a[6], a[5], false, n, &x);
+    if (n == 0) return;
+    if (t.size(0) == 0) refuse_shape("logits", "of at least one row");
+    const OnDevice on(s, a[7]);
+    call("cb_logprobs", [&] { return g_lib.logprobs(c, &x, on.stream); });
+}
+// handle, shape, logits, accepted, top_k, res, stream
+void do_accept_logprobs(PyObject* const* a) {
+    cb_ctx* c = ctx_of(a[0]);
+    const Shape s = shape_of(a[1]);
+    cb_logprobs_args x = {};
+    const at::Tensor& t = tensor_of(a[2]);
+    logits_dtype_of(s, t);
+    x.logits = logits_of(a[2], &x.logits_dtype, &x.logits_row_stride);
+    if (t.size(0) != s.B || t.size(1) != s.T || t.size(2) != s.V) refuse_shape("logits", "[batch, max_nodes, vocab]");
+    Ref nodes(PyObject_GetItem(a[3], s_accept_nodes)), toks(PyObject_GetItem(a[3], s_out_tokens));
+    const int32_t* an = static_cast<int32_t*>(arg(s, nodes.o, "accept_nodes", at::kInt, {s.B, s.Dmax}, "[batch, max_depth]").p);
+    const int32_t* ot = static_cast<int32_t*>(arg(s, toks.o, "out_tokens", at::kInt, {s.B, s.Dmax + 1}, "[batch, max_depth + 1]").p);
+    likely_of(s, a[5], a[4], true, 0, &x);
+    const OnDevice on(s, a[6]);
+    call("cb_accept_logprobs", [&] { return g_lib.accept_logprobs(c, an, ot, &x, on.stream); });
+}
+
 // set_library(CachebackError, {name: address})
 PyObject* set_library(PyObject*, PyObject* args) {
     PyObject *err, *addr;
@@ -268,7 +490,9 @@ PyObject* set_library(PyObject*, PyObject* args) {
     Library l;
     if (!(take("cb_reset", &l.reset) && take("cb_update", &l.update) && take("cb_update_bulk", &l.update_bulk) && take("cb_draft_tree", &l.draft_tree) &&
           take("cb_update_draft_tree", &l.update_draft_tree) && take("cb_tree_attn", &l.tree_attn) && take("cb_accept", &l.accept) &&
-          take("cb_accept_update_draft_tree", &l.accept_update_draft_tree) && take("cb_kv_commit", &l.kv_commit) && take("cb_status_str", &l.status_str)))
+          take("cb_accept_update_draft_tree", &l.accept_update_draft_tree) && take("cb_kv_commit", &l.kv_commit) && take("cb_chunk_append", &l.chunk_append) &&
+          take("cb_chunk_attn", &l.chunk_attn) && take("cb_tree_rope", &l.tree_rope) && take("cb_logprobs", &l.logprobs) &&
+          take("cb_accept_logprobs", &l.accept_logprobs) && take("cb_status_str", &l.status_str)))
         return nullptr;
     g_lib = l;
     Py_INCREF(err);
@@ -281,7 +505,9 @@ PyMethodDef g_methods[] = {
     {"set_library", set_library, METH_VARARGS, nullptr},
     CB_FAST("reset", 3, do_reset), CB_FAST("update", 5, do_update<false>), CB_FAST("update_bulk", 5, do_update<true>), CB_FAST("draft_tree", 5, do_draft),
     CB_FAST("update_draft_tree", 6, do_update_draft), CB_FAST("accept", 6, do_accept), CB_FAST("accept_update_draft_tree", 8, do_accept_update_draft),
-    CB_FAST("tree_attn", 15, do_attn), CB_FAST("kv_commit", 10, do_kv_commit), {nullptr, nullptr, 0, nullptr}};
+    CB_FAST("tree_attn", 15, do_attn), CB_FAST("kv_commit", 10, do_kv_commit), CB_FAST("chunk_append", 17, do_chunk_append),
+    CB_FAST("tree_rope", 16, do_tree_rope), CB_FAST("chunk_attn", 14, do_chunk_attn), CB_FAST("logprobs", 8, do_logprobs),
+    CB_FAST("accept_logprobs", 7, do_accept_logprobs), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -88,6 +88,7 @@ extern "C" cb_status cb_chunk_attn(cb_ctx* ctx, const cb_chunk_attn_args* a, voi
     p.scale_log2 = scale * 1.4426950408889634f;
     p.status = ctx->d_status;
     cudaStream_t st = (cudaStream_t)stream;
+    if (!(c.flags & CB_FLAG_ATTN_CUDA_CORES)) return cb_chunk_launch_tensor(ctx, p, st);
     const long long blocks = ((long long)p.n_rows * p.Hq + kWarps - 1) / kWarps;
     if (blocks > 0x7FFFFFFFll) return CB_ERR_UNSUPPORTED;
     if (p.D == 128) cb_chunk_cc_kernel<128><<<(unsigned)blocks, 32 * kWarps, 0, st>>>(p);

@@ -27,6 +27,14 @@ struct CbChunkParams {
     int max_chunk, max_keys;  // bounds of a sequence's new tokens and of all its tokens
     float scale_log2;         // softmax scale * log2(e)
     uint32_t* status;
+    // the tensor-core kernel's split (cb_chunk_sched.cuh)
+    int NPT;                  // tokens per row tile = 128 / G
+    uint32_t g_inv;           // x / G = x * g_inv >> 16 for x < 256
+    int one;                  // every chunk fits one row tile, by max_chunk
+    int nc;                   // persistent CTAs
+    int w1, w2, d1, d2;       // positions per key tile of a unit with one or two row tiles, and which of them decides whose tile it is
+    float* part;              // partial outputs of units shared between CTAs; tickets and turn as in tree attention, whose scratch this is
+    uint32_t *part_ticket, *part_turn;
 };
 
 // A sequence's chunk as attention sees it.  n = 0: nothing to do, or nothing that may be done (error: why).
@@ -40,3 +48,5 @@ __device__ __forceinline__ CbChunkSeq cb_chunk_seq(const CbChunkParams& p, int b
     else { s.n = q1 - q0; s.ctx = ctx; }
     return s;
 }
+
+cb_status cb_chunk_launch_tensor(cb_ctx* ctx, const CbChunkParams& p, cudaStream_t st);

@@ -1,0 +1,163 @@
+"""Chunk attention's split over the persistent CTAs and the search for a row's sequence, from the kernels' own headers compiled for the host (a
+warp's 32 lanes emulated), against a plain restatement."""
+import os
+import subprocess
+
+import numpy as np
+import pytest
+
+from tests.test_attn_schedule_pairs import _SHIM as _WARP
+
+_SHIM = _WARP.split('#include "cb_attn_sched32.cuh"')[0] + r"""
+inline int __clz(int x) { return x == 0 ? 32 : __builtin_clz((unsigned)x); }
+#include "cb_chunk_sched.cuh"
+int main() {
+    int what;
+    while (scanf("%d", &what) == 1) {
+        if (what == 0) {                                       // sequences of rows
+            int B, n;
+            if (scanf("%d %d", &B, &n) != 2) return 1;
+            std::vector<int> q(B + 1);
+            for (int& x : q) if (scanf("%d", &x) != 1) return 1;
+            for (int r = 0; r < n; ++r) {
+                int got = -2, other = -2;
+                warp([&](int lane) { const int b = cb_find_sequence(q.data(), B, r, lane); if (lane == 0) got = b; if (lane == 31) other = b; });
+                if (got != other) { printf("lanes differ\n"); return 1; }
+                printf("%d ", got);
+            }
+        } else if (what == 1) {
+            long long n, a, b;
+            if (scanf("%lld %lld %lld", &n, &a, &b) != 3) return 1;
+            printf("%lld ", cb_floor_sum(n, a, b));
+        } else {
+            CbChunkParams p = {};
+            if (scanf("%d %d %d %d %d %d %d %d", &p.B, &p.G, &p.Hkv, &p.D, &p.nc, &p.max_chunk, &p.max_keys, &p.n_rows) != 8) return 1;
+            std::vector<int> q(p.B + 1), c(p.B);
+            for (int& x : q) if (scanf("%d", &x) != 1) return 1;
+            for (int& x : c) if (scanf("%d", &x) != 1) return 1;
+            p.q_start = q.data(); p.ctx_len = c.data();
+            p.NPT = CB_MT / p.G; p.one = p.max_chunk <= p.NPT;
+            CbAttnParams w = {};
+            w.D = p.D;
+            cb_attn_weights(w);
+            p.w1 = w.w1; p.w2 = w.w2; p.d1 = w.d1; p.d2 = w.d2;
+            int error = 0;
+            for (int k = 0; k < p.nc; ++k) {
+                CbChunkWalker wk = {};
+                long long tot = 0;
+                warp([&](int lane) {
+                    CbChunkWalker x;
+                    int err = 0;
+                    const long long t = cb_chunk_range(p, k, lane, &x, &err);
+                    if (err) error = err;
+                    if (lane == 7) { wk = x; tot = t; }
+                });
+                CbChunkUnit u;
+                while (wk.next(p, &u)) {
+                    const CbChunkShape& s = wk.s;
+                    const int tiles = s.tiles(u.rg), wt = s.wt(u.rg), cf = cb_cta_of(tot, p.nc, u.first);
+                    const int np = tot >= (long long)p.nc * wt ? cb_cta_of(tot, p.nc, u.first + (long long)(tiles - 1) * wt) - cf + 1 : tiles;
+                    printf("%d %d %d %d %d %d %d %d %d %d %d %d ", k, u.b, u.kh, u.rg, u.t0, u.t1, tiles, s.two_rows(u.rg) ? 2 : 1, s.row0, s.end(u.rg), cf, np);
+                }
+            }
+            printf("\n%d", error);
+        }
+        printf("\n");
+    }
+}
+"""
+
+
+@pytest.fixture(scope="module")
+def shim(tmp_path_factory):
+    from paper_2511_21699_b200 import build as b
+    d = tmp_path_factory.mktemp("chunk")
+    (d / "shim.cpp").write_text(_SHIM)
+    cuda = os.path.dirname(os.path.dirname(os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")))
+    subprocess.check_call(["g++", "-O1", "-std=c++17", "-w", "-I", os.path.join(cuda, "include"), "-I", os.path.join(b.ROOT, "include"), "-I", b.CSRC,
+                           str(d / "shim.cpp"), "-o", str(d / "shim")])
+
+    def run(text):
+        r = subprocess.run([str(d / "shim")], input=text, capture_output=True, text=True, timeout=120)
+        assert r.returncode == 0, (r.returncode, r.stdout[-200:])
+        return r.stdout
+    return run
+
+
+@pytest.mark.parametrize("B", [1, 2, 31, 32, 33, 100, 1024, 1025, 2500])
+def test_sequence_of_a_row(shim, B):
+    rng = np.random.default_rng(B)
+    n = np.where(rng.random(B) < 0.5, 0, rng.integers(0, 4, B))
+    q = 3 + np.concatenate([[0], np.cumsum(n)])
+    rows = int(q[-1]) + 4
+    got = np.array(shim("0 %d %d %s\n" % (B, rows, " ".join(map(str, q)))).split(), int)
+    assert np.array_equal(got, np.searchsorted(q[:-1], np.arange(rows), side="right") - 1)
+
+
+def test_floor_sum(shim):
+    rng = np.random.default_rng(0)
+    cases = [(0, 5, 7), (1, 0, 0), (1, 256, 300), (3, 128, 127)] + [(int(rng.integers(0, 400)), int(rng.choice([16, 18, 32, 36, 42, 50, 64, 84, 128, 256])),
+                                                                     int(rng.integers(0, 40000))) for _ in range(200)]
+    got = [int(x) for x in shim("".join("1 %d %d %d\n" % c for c in cases)).split()]
+    assert got == [sum((a * i + b) // 128 for i in range(n)) for n, a, b in cases]
+
+
+def _plain(G, hkv, D, nc, max_chunk, q, ctx):
+    """[(cta, b, kh, rg, t0, t1, tiles, row tiles, first row, keys seen, cta of the first tile, ctas)], tile by tile."""
+    npt = 128 // G
+    one = max_chunk <= npt
+    tg = npt if one else 2 * npt
+    w = {128: {1: (4, 3), 2: (6, 2)}, 64: {1: (1, 0), 2: (2, 0)}}[D]
+    units, at = [], 0
+    for b in range(len(ctx)):
+        n = q[b + 1] - q[b]
+        for rg in range(-(-n // tg)):
+            nrt = 2 if not one and n - rg * tg > npt else 1
+            wt, dec = w[nrt]
+            pad = 3 * wt if nrt == 2 else 2 * wt
+            end = ctx[b] + min(n, (rg + 1) * tg)
+            tiles = -(-end // 128)
+            for kh in range(hkv):
+                units.append((b, kh, rg, nrt, q[b], end, tiles, wt, at + pad + dec))
+                at += pad + tiles * wt
+    bounds = [at * c // nc for c in range(nc + 1)]
+    out = []
+    for b, kh, rg, nrt, row0, end, tiles, wt, first in units:
+        owner = np.searchsorted(bounds, first + wt * np.arange(tiles), side="right") - 1
+        holders = np.unique(owner)
+        for c in holders:
+            mine = np.nonzero(owner == c)[0]
+            out.append((int(c), b, kh, rg, int(mine[0]), int(mine[-1]) + 1, tiles, nrt, row0, end, int(owner[0]), len(holders)))
+    return sorted(out)
+
+
+@pytest.mark.parametrize("G,hkv,D,new,ctx", [
+    (1, 32, 128, [1], [4095]), (4, 8, 128, [1] * 64, list(range(120, 8200, 128))), (4, 4, 64, [0, 509, 1, 64, 0, 200], [3, 0, 5000, 640, 9, 0]),
+    (8, 8, 128, [8192], [0]), (7, 4, 128, [1000, 3, 18, 19, 36, 37], [77, 0, 5, 250, 1, 128]), (5, 1, 64, [2000, 1], [31, 9000]), (16, 3, 128, [40, 8, 9], [0, 1, 2]),
+    (3, 2, 64, [0, 0, 0], [1, 2, 3]), (1, 1, 128, [1], [0]), (2, 2, 128, [300] * 3, [0, 128, 500]), (1, 40, 64, [129, 128, 127, 1], [0, 0, 0, 0]),
+    (4, 1, 128, [1] * 100, [5] * 100),
+])
+def test_who_works_on_what(shim, G, hkv, D, new, ctx):
+    q = np.concatenate([[0], np.cumsum(new)]).tolist()
+    for nc in (148, 160, 7, 1):
+        for max_chunk in sorted({max(max(new), 1), max(q[-1], 1)}):
+            text = "2 %d %d %d %d %d %d %d %d %s %s\n" % (len(new), G, hkv, D, nc, max_chunk, 1 << 30, q[-1], " ".join(map(str, q)), " ".join(map(str, ctx)))
+            units, error = shim(text).split("\n")[:2]
+            got = sorted(tuple(int(y) for y in x) for x in np.array(units.split(), np.int64).reshape(-1, 12))
+            assert int(error) == 0
+            assert got == _plain(G, hkv, D, nc, max_chunk, q, ctx)
+            have = sorted((x[1], x[2], x[3], t) for x in got for t in range(x[4], x[5]))    # every tile once
+            assert len(have) == len(set(have)) == sum(x[6] for x in {(y[1], y[2], y[3]): y for y in got}.values())
+
+
+def test_sequences_that_are_left_out(shim):
+    from paper_2511_21699_b200 import _lib
+    for q, ctx, left, code in (([0, 3, 5, 9], [1, -1, 2], 1, _lib.CB_ERR_INVALID_ARG), ([0, 3, 2, 9], [1, 1, 2], (1, 2), _lib.CB_ERR_INVALID_ARG),   # seven tokens are more than max_chunk
+                              
+                               ([0, 3, 5, 99], [1, 1, 2], 2, _lib.CB_ERR_INVALID_ARG), ([-2, 3, 5, 9], [1, 1, 2], 0, _lib.CB_ERR_INVALID_ARG),
+                               ([0, 3, 5, 9], [1, 999, 2], 1, _lib.CB_ERR_KV_FULL), ([0, 3, 5, 9], [1, 1, 2 ** 31 - 1], 2, _lib.CB_ERR_KV_FULL),
+                               ([0, 6, 7, 9], [1, 1, 2], 0, _lib.CB_ERR_INVALID_ARG)):
+        text = "2 3 1 2 64 148 5 1000 9 %s %s\n" % (" ".join(map(str, q)), " ".join(map(str, ctx)))
+        units, error = shim(text).split("\n")[:2]
+        got = {int(x[1]) for x in np.array(units.split(), np.int64).reshape(-1, 12)}
+        assert int(error) == code and got == {0, 1, 2} - set(np.atleast_1d(left).tolist())

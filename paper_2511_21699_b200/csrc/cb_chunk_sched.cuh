@@ -4,31 +4,70 @@
 // group of two 128-row tiles (one where the last group has no more, or all chunks fit one), and all units laid end to end, with padding in
 // front of each for what starting it costs, are cut into equal ranges.  What differs: a row group sees the keys up to its own last token, so
 // the units of one sequence grow along its chunk, and a chunk may have hundreds of row groups.  The order is (sequence, row group, kv head);
-// where a sequence's row groups start is a sum of floor((a k + b) / 128) over k, which has a closed form by Euclid's steps, so that a CTA
-// finds its first unit by a scan over the sequences and a search in one of them.
+// where a sequence's row groups start is a sum of floor((a k + b) / 128) over k, which has a closed form, so that a CTA
+// finds its first unit by a scan over the sequences and a search in one of them.  (A first form, with 64-bit divisions and lengths read twice, held
+// the first copy of a launch up by 8 k cycles at batch 1 and 19 k for an 8 k prompt.)
 #pragma once
 #include "cb_attn.cuh"
 #include "cb_chunk.cuh"
 
-// sum over i < n of floor((a i + b) / 128), a, b >= 0: whole multiples are taken out, what is left counts the lattice points under a line, which
-// are the same with the axes exchanged.
-__device__ __forceinline__ long long cb_floor_sum(long long n, long long a, long long b) {
-    long long sum = 0, m = 128;
+// sum over i < n of floor((a i + b) / 128), a in 1..256, b >= 0.  Everything a launch does waits for this, so divisions (a chain of 100 to 200
+// cycles in 32 bits, several times that in 64) are for the head counts that need them:
+//   a a multiple of 128: every term is floor(b / 128) + i a / 128;
+//   a a smaller power of two, m = 128 / a: floor((a i + b) / 128) = floor((i + c) / m) with c = floor(b / a), a sum of runs of m equal terms;
+//   otherwise Euclid's steps: whole multiples are taken out, what is left counts the lattice points under a line, which are the same with the
+//   axes exchanged.
+__device__ __forceinline__ long long cb_floor_sum(long long n, int a, int b) {
+    if (n <= 0) return 0;
+    if ((a & 127) == 0) return (a >> 7) * (n * (n - 1) / 2) + n * (b >> 7);
+    if ((a & (a - 1)) == 0) {
+        const int la = 31 - __clz(a), lm = 7 - la;
+        auto runs = [&](long long x) { const long long q = x >> lm; return ((q * (q - 1) / 2) << lm) + q * (x & ((1 << lm) - 1)); };   // of floor(j / m), j < x
+        const long long c = b >> la;
+        return runs(n + c) - runs(c);
+    }
+    long long sum = 0;
+    uint32_t m = 128, x = (uint32_t)a, y = (uint32_t)b;
     while (true) {
-        if (a >= m) { sum += (n - 1) * n / 2 * (a / m); a %= m; }
-        if (b >= m) { sum += n * (b / m); b %= m; }
-        const long long y = a * n + b;
-        if (y < m) return sum;
-        n = y / m; b = y % m;
-        const long long t = m; m = a; a = t;
+        sum += (n - 1) * n / 2 * (x / m) + n * (y / m);
+        x %= m; y %= m;
+        const unsigned long long top = (unsigned long long)x * n + y;
+        if (top < m) return sum;
+        n = (long long)cb_div((long long)top, m);
+        y = (uint32_t)(top - (unsigned long long)n * m);
+        const uint32_t t = m; m = x; x = t;
     }
 }
 
+// The ranges of the CTAs: range c starts at floor(total c / nc).  Positions below 2^32 (a call of 2^25 tiles) need one division.
+struct CbChunkCuts {
+    long long total;
+    int nc;
+    uint32_t q, r;            // total = q nc + r, in 32 bits
+    bool small;
+    __device__ __forceinline__ void init(long long t, int n) {
+        total = t; nc = n; small = t >> 32 == 0;
+        q = (uint32_t)t / (uint32_t)n; r = (uint32_t)t - q * (uint32_t)n;
+    }
+    __device__ __forceinline__ long long start(int c) const {
+        if (!small) return total * c / nc;
+        return (long long)((unsigned long long)q * (uint32_t)c) + cb_quot((long long)(r * (uint32_t)c), nc);   // r c < nc^2
+    }
+    // the range that holds position x < total
+    __device__ __forceinline__ int of(long long x) const {
+        if (!small) return cb_cta_of(total, nc, x);
+        int c = min(max((int)(__fdividef((float)x, (float)total) * (float)nc), 0), nc - 1);      // off by one at most
+        while (c > 0 && start(c) > x) --c;
+        while (c + 1 < nc && start(c + 1) <= x) ++c;
+        return c;
+    }
+};
+
 struct CbChunkShape {
-    int row0, n, ctx, error;
-    int mtn, RG, tg;          // row tiles, row groups, tokens per row group
-    int w1, w2, d1, d2;
-    bool one;
+    int row0 = 0, n = 0, ctx = 0, error = 0;
+    int mtn = 0, RG = 0, tg = 0;   // row tiles, row groups, tokens per row group
+    int w1 = 0, w2 = 0, d1 = 0, d2 = 0;
+    bool one = false;
     __device__ __forceinline__ int end(int rg) const { return ctx + min(n, (rg + 1) * tg); }                 // keys that row group rg sees
     __device__ __forceinline__ int tiles(int rg) const { return (end(rg) + CB_KT - 1) / CB_KT; }
     __device__ __forceinline__ bool two_rows(int rg) const { return !one && mtn - 2 * rg >= 2; }
@@ -40,7 +79,7 @@ struct CbChunkShape {
     __device__ __forceinline__ long long before(int r) const {
         if (r <= 0) return 0;
         const int k = min(r, RG - 1);
-        return w2 * (cb_floor_sum(k, tg, (long long)ctx + tg + CB_KT - 1) + 3ll * k) + (r == RG ? unit(RG - 1) : 0);
+        return w2 * (cb_floor_sum(k, tg, ctx + tg + CB_KT - 1) + 3ll * k) + (r == RG ? unit(RG - 1) : 0);
     }
     __device__ __forceinline__ long long weight(int Hkv) const { return RG > 0 ? Hkv * before(RG) : 0; }
 };
@@ -88,60 +127,95 @@ struct CbChunkWalker {
     }
 };
 
-// This CTA's range and the walker at its start, by a whole warp (every lane gets both); returns the positions of all units.  *error: what this
-// lane found wrong with a sequence, or 0.
-__device__ __forceinline__ long long cb_chunk_range(const CbChunkParams& p, int cta, int lane, CbChunkWalker* w, int* error) {
-    long long tot = 0, mine = 0;
-    int err = 0;
-    CbChunkShape first = {};
-    for (int base = 0; base < p.B; base += 32) {
-        CbChunkShape s = {};
-        if (base + lane < p.B) s = cb_chunk_shape(p, base + lane);
-        if (base == 0) first = s;
-        if (s.error) err = s.error;
-        mine += s.weight(p.Hkv);
+// This CTA's range and the walker at its start, by a whole warp (every lane gets both), and the cuts.  *error: what this lane found wrong with a
+// sequence, or 0.
+__device__ __forceinline__ void cb_chunk_range(const CbChunkParams& p, int cta, int lane, CbChunkWalker* w, CbChunkCuts* cuts, int* error) {
+    auto shape = [&](int b) { return b < p.B ? cb_chunk_shape(p, b) : CbChunkShape{}; };
+    CbChunkShape s = shape(lane);
+    long long own = s.weight(p.Hkv), tot = own;
+    int err = s.error;
+    for (int b = 32 + lane; b - lane < p.B; b += 32) {
+        const CbChunkShape t = shape(b);
+        if (t.error) err = t.error;
+        tot += t.weight(p.Hkv);
     }
-    tot = mine;
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) tot += __shfl_xor_sync(CB_FULL, tot, o);
     *error = err;
-    w->g = cb_range_start(tot, p.nc, cta);
-    w->g1 = cb_range_start(tot, p.nc, cta + 1);
-    if (w->g >= w->g1) return tot;
+    if (p.B == 1) {                                           // lane 0 has all of it
+        tot = __shfl_sync(CB_FULL, tot, 0);
+    } else {
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) tot += __shfl_xor_sync(CB_FULL, tot, o);
+    }
+    cuts->init(tot, p.nc);
+    w->g = cuts->start(cta);
+    w->g1 = cuts->start(cta + 1);
+    if (w->g >= w->g1) return;
     long long run = 0;
-    for (int base = 0; base < p.B; base += 32) {
-        CbChunkShape s = first;
-        if (base > 0) {
-            s = CbChunkShape{};
-            if (base + lane < p.B) s = cb_chunk_shape(p, base + lane);
-        }
-        const long long own = s.weight(p.Hkv);
+    int base = 0, l = 0;
+    while (p.B > 1) {                                         // ends at the sequence that holds g
         long long inc = own;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
             const long long t = __shfl_up_sync(CB_FULL, inc, o);
             if (lane >= o) inc += t;
         }
-        const long long pre = run + inc - own;
-        const uint32_t hit = __ballot_sync(CB_FULL, own > 0 && w->g >= pre && w->g < pre + own);
+        const uint32_t hit = __ballot_sync(CB_FULL, w->g < run + inc);
         if (hit) {
-            const int l = __ffs(hit) - 1;
-            w->b = base + l;
-            w->pos = __shfl_sync(CB_FULL, pre, l);
+            l = __ffs(hit) - 1;
+            run = __shfl_sync(CB_FULL, run + inc - own, l);
             break;
         }
         run += __shfl_sync(CB_FULL, inc, 31);
+        base += 32;
+        if (base >= p.B) { w->g = w->g1; return; }            // (the lengths have changed under us)
+        s = shape(base + lane);
+        own = s.weight(p.Hkv);
     }
-    w->s = cb_chunk_shape(p, w->b);
-    const long long off = w->g - w->pos;
-    int lo = 0, hi = w->s.RG - 1;                             // the last row group that starts no later
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) / 2;
-        if (w->s.before(mid) * p.Hkv <= off) lo = mid; else hi = mid - 1;
+    w->b = base + l;
+    // that lane's shape for all
+    s.row0 = __shfl_sync(CB_FULL, s.row0, l); s.n = __shfl_sync(CB_FULL, s.n, l); s.ctx = __shfl_sync(CB_FULL, s.ctx, l);
+    s.mtn = __shfl_sync(CB_FULL, s.mtn, l); s.RG = __shfl_sync(CB_FULL, s.RG, l);
+    s.tg = p.one ? p.NPT : 2 * p.NPT; s.one = p.one != 0;
+    s.w1 = p.w1; s.w2 = p.w2; s.d1 = p.d1; s.d2 = p.d2;
+    w->s = s;
+    // the last row group that starts no later: 32 candidates at a time
+    const long long off = w->g - run;
+    int lo = 0, n = s.RG;                                     // it is in [lo, lo + n)
+    while (n > 1) {
+        const int step = (n + 31) / 32, at = lo + lane * step;
+        const uint32_t hit = __ballot_sync(CB_FULL, lane * step < n && s.before(at) * p.Hkv <= off);
+        const int k = 31 - __clz(hit);
+        n = min(step, n - k * step);
+        lo += k * step;
     }
-    const long long at = w->s.before(lo) * p.Hkv;
+    const long long at = s.before(lo) * p.Hkv;
     w->rg = lo;
-    w->kh = (int)cb_div(off - at, w->s.unit(lo));
-    w->pos += at + (long long)w->kh * w->s.unit(lo);
-    return tot;
+    w->kh = (int)cb_quot(off - at, s.unit(lo));
+    w->pos = run + at + (long long)w->kh * s.unit(lo);
+}
+
+// Launches of few units of one row tile (single tokens of a small batch) are not cut into ranges: unit u = (sequence, kv head) has CTAs
+// u cs .. u cs + cs - 1, which take equal parts of its tiles.  A CTA then needs one sequence's lengths and next to no arithmetic before its
+// first copy, and no CTA has more than one unit to see to.
+__device__ __forceinline__ bool cb_chunk_share(const CbChunkParams& p, int cta, CbChunkUnit* u, CbChunkShape* s, int* ctas) {
+    const int unit = cta / p.cs, rank = cta - unit * p.cs;
+    u->b = unit / p.Hkv; u->kh = unit - u->b * p.Hkv; u->rg = 0;
+    *s = cb_chunk_shape(p, u->b);
+    if (s->RG == 0) return false;
+    const int tiles = s->tiles(0);
+    *ctas = min(p.cs, tiles);
+    if (rank >= *ctas) return false;
+    u->t0 = (int)((long long)tiles * rank / *ctas); u->t1 = (int)((long long)tiles * (rank + 1) / *ctas);
+    return true;
+}
+// How many CTAs share a unit: what the longest unit's share of tiles takes, bandwidth shared by all, and what putting the parts together
+// adds (in tiles; some 0.2 each), against equal ranges, whose schedule and merging take some 6 tiles longer.  0: equal ranges.
+inline int cb_chunk_pick_share(long long units, long long tiles, int num_ctas) {
+    int best = 0;
+    double least = (double)units * (double)(tiles + 2) / num_ctas + 6.0;
+    for (int cs = 1; cs <= 32 && units * cs <= num_ctas; ++cs) {
+        const double cost = (double)((tiles + cs - 1) / cs) + 0.2 * cs;
+        if (cost < least) { least = cost; best = cs; }
+    }
+    return best;
 }

@@ -125,6 +125,12 @@ __global__ void __launch_bounds__(kThreads, 1) cb_chunk_tc_kernel(const CbChunkP
             const bool isV = warp == 3;
             constexpr uint32_t GROUP = 1024 * C::DB;          // bytes of 8 keys
             const bool active = lane < 8;
+            if (isV) {
+                // The block table into L2, a slice per CTA, while the units are worked out: the first copies' addresses come from it.
+                const long long lines = ((long long)p.B * p.max_pages * 4 + 127) / 128;
+                for (long long k = (long long)cta * 32 + lane, n = 0; k < lines && n < 4; k += (long long)gridDim.x * 32, ++n)
+                    asm volatile("prefetch.global.L2 [%0];" ::"l"(reinterpret_cast<const char*>(p.block_table) + k * 128));
+            }
             for (uint32_t uq = 0; (ok = mbar_wait(bar_ufull(uq % kUnitRing), (uq / kUnitRing) & 1, s_abort, p.status)); ++uq) {
                 const volatile ChunkUnit* u = &s_units[uq % kUnitRing];
                 if (u->nrt == 0) break;
@@ -202,53 +208,82 @@ __global__ void __launch_bounds__(kThreads, 1) cb_chunk_tc_kernel(const CbChunkP
             }
         } else {
             // ------------------------------------------------------------------ units for all roles, query tiles
-            // The set of tickets that this launch counts in; the other one is cleared for the next launch (see cb_attn_tc.cu).
-            const int ticket_set = (int)(*reinterpret_cast<volatile uint32_t*>(p.part_turn) & 1u) * CB_ATTN_TICKETS;
-            if (lane < 16) p.part_ticket[CB_ATTN_TICKETS - ticket_set + cta * 16 + lane] = 0u;
-            CbChunkWalker wk;
-            int error = 0;
-            const long long tot = cb_chunk_range(p, cta, lane, &wk, &error);
-            if (cta == 0 && error) atomicCAS(p.status, 0u, (uint32_t)error);
-            if (lane == 0) {
-                *s_tot = tot;
-                uint32_t uq = 0;
-                int seq = 0;
-                CbChunkUnit x;
-                while (ok && wk.next(p, &x)) {
-                    volatile ChunkUnit* u = &s_units[uq % kUnitRing];
-                    const CbChunkShape& s = wk.s;             // of the unit's sequence: the walker goes on when it is asked again
-                    const int tiles = s.tiles(x.rg), nrt = s.two_rows(x.rg) ? 2 : 1, wt = s.wt(x.rg);
-                    u->b = x.b; u->kh = x.kh; u->rg = x.rg; u->t0 = x.t0; u->t1 = x.t1; u->tiles = tiles; u->nrt = nrt;
-                    u->row0 = s.row0; u->n = s.n; u->ctx = s.ctx; u->end = s.end(x.rg);
-                    u->seq0 = seq;
-                    u->skip = nrt == 2 && x.t1 == tiles && x.t1 - x.t0 > 1 && (tiles - 1) * CB_KT >= s.ctx + (2 * x.rg + 1) * p.NPT;
-                    u->dirty = max((s.end(x.rg) + 15) / 16 * 16 - (s.ctx + s.n), 0);
-                    seq += 2 * (x.t1 - x.t0);
-                    if (!(x.t0 == 0 && x.t1 == tiles)) {
-                        // Shared with other CTAs: who holds its first tile, and how many there are (with ranges of at least one tile's positions the
-                        // CTAs from the first tile's to the last one's; shorter ranges hold the deciding position of one tile at most).
-                        const int cf = cb_cta_of(tot, p.nc, x.first);
-                        const bool wide = tot >= (long long)p.nc * wt;
-                        u->cf = cf;
-                        u->np = wide ? cb_cta_of(tot, p.nc, x.first + (long long)(tiles - 1) * wt) - cf + 1 : tiles;
-                        u->xpos = wide ? -1 : (int)x.first;
-                        u->wt = wt;
-                        u->ticket = ticket_set + cf * 16;
-                    }
-                    mbar_arrive(bar_ufull(uq % kUnitRing));
-                    if (uq > 0 && !(ok = mbar_wait(bar_qfree, (uq - 1) & 1, s_abort, p.status))) break;
-                    mbar_expect_tx(bar_qfull, (uint32_t)(nrt * C::DB * RT * 128));
-                    for (int k = 0; k < nrt; ++k)
-                        for (int db = 0; db < C::DB; ++db)
-                            tma_load_4d(sbase + C::OFF_Q + k * C::Q_BYTES + db * (CB_MT * 128), &maps.q, bar_qfull, db * 64, x.kh * p.G,
-                                        u->row0 + (2 * x.rg + k) * p.NPT, 0);
+            // The set of tickets that this launch counts in; the other one is cleared below, for the next launch (see cb_attn_tc.cu).
+            uint32_t turn;
+            asm volatile("ld.volatile.global.u32 %0, [%1];" : "=r"(turn) : "l"(p.part_turn));
+            const int ticket_set = (int)(turn & 1u) * CB_ATTN_TICKETS;
+            int error = 0, seq = 0;
+            uint32_t uq = 0;
+            // What all roles need of a unit; a shared one's holder of the first tile and number of CTAs are set before.
+            auto publish = [&](const CbChunkUnit& x, const CbChunkShape& s) {
+                volatile ChunkUnit* u = &s_units[uq % kUnitRing];
+                const int tiles = s.tiles(x.rg), nrt = s.two_rows(x.rg) ? 2 : 1;
+                u->b = x.b; u->kh = x.kh; u->rg = x.rg; u->t0 = x.t0; u->t1 = x.t1; u->tiles = tiles; u->nrt = nrt;
+                u->row0 = s.row0; u->n = s.n; u->ctx = s.ctx; u->end = s.end(x.rg);
+                u->seq0 = seq;
+                u->skip = nrt == 2 && x.t1 == tiles && x.t1 - x.t0 > 1 && (tiles - 1) * CB_KT >= s.ctx + (2 * x.rg + 1) * p.NPT;
+                u->dirty = max((s.end(x.rg) + 15) / 16 * 16 - (s.ctx + s.n), 0);
+                seq += 2 * (x.t1 - x.t0);
+                mbar_arrive(bar_ufull(uq % kUnitRing));
+            };
+            auto load_queries = [&](const CbChunkUnit& x, const CbChunkShape& s) {
+                const int nrt = s.two_rows(x.rg) ? 2 : 1;
+                mbar_expect_tx(bar_qfull, (uint32_t)(nrt * C::DB * RT * 128));
+                for (int k = 0; k < nrt; ++k)
+                    for (int db = 0; db < C::DB; ++db)
+                        tma_load_4d(sbase + C::OFF_Q + k * C::Q_BYTES + db * (CB_MT * 128), &maps.q, bar_qfull, db * 64, x.kh * p.G, s.row0 + (2 * x.rg + k) * p.NPT, 0);
+            };
+            CbChunkUnit x;
+            if (p.cs > 0) {
+                CbChunkShape s;
+                int np = 0;
+                const bool has = cb_chunk_share(p, cta, &x, &s, &np);
+                error = s.error;
+                if (lane == 0 && has) {
+                    volatile ChunkUnit* u = &s_units[0];
+                    const int cf = cta / p.cs * p.cs;
+                    u->cf = cf; u->np = np; u->xpos = -1; u->ticket = ticket_set + cf * 16;
+                    publish(x, s);
+                    load_queries(x, s);
                     ++uq;
                 }
-                if (ok) {
-                    s_units[uq % kUnitRing].nrt = 0;
-                    mbar_arrive(bar_ufull(uq % kUnitRing));
+            } else {
+                CbChunkWalker wk;
+                CbChunkCuts cuts;
+                cb_chunk_range(p, cta, lane, &wk, &cuts, &error);
+                if (cta > 0) error = 0;
+                if (lane == 0) {
+                    *s_tot = cuts.total;
+                    while (ok && wk.next(p, &x)) {
+                        const CbChunkShape& s = wk.s;         // of the unit's sequence: the walker goes on when it is asked again
+                        const int tiles = s.tiles(x.rg), wt = s.wt(x.rg);
+                        if (!(x.t0 == 0 && x.t1 == tiles)) {
+                            // Shared with other CTAs: who holds its first tile, and how many there are (with ranges of at least one tile's positions the
+                            // CTAs from the first tile's to the last one's; shorter ranges hold the deciding position of one tile at most).
+                            volatile ChunkUnit* u = &s_units[uq % kUnitRing];
+                            const int cf = cuts.of(x.first);
+                            const bool wide = cuts.total >= (long long)p.nc * wt;
+                            u->cf = cf;
+                            u->np = wide ? cuts.of(x.first + (long long)(tiles - 1) * wt) - cf + 1 : tiles;
+                            u->xpos = wide ? -1 : (int)x.first;
+                            u->wt = wt;
+                            u->ticket = ticket_set + cf * 16;
+                        }
+                        publish(x, s);
+                        if (uq > 0 && !(ok = mbar_wait(bar_qfree, (uq - 1) & 1, s_abort, p.status))) break;
+                        load_queries(x, s);
+                        ++uq;
+                    }
                 }
             }
+            if (lane == 0 && ok) {
+                s_units[uq % kUnitRing].nrt = 0;
+                mbar_arrive(bar_ufull(uq % kUnitRing));
+            }
+            __syncwarp();
+            for (int k = cta; k < p.nc; k += gridDim.x)       // a grid of few CTAs clears the others' too
+                if (lane < 16) p.part_ticket[CB_ATTN_TICKETS - ticket_set + k * 16 + lane] = 0u;
+            if (error) atomicCAS(p.status, 0u, (uint32_t)error);
         }
         __syncwarp();
     } else {
@@ -504,9 +539,10 @@ __global__ void __launch_bounds__(kThreads, 1) cb_chunk_tc_kernel(const CbChunkP
                     float* const own = slot_of(cta, t0 == 0);
                     auto load_part = [&](float4* v, const float* pp, int e) {
 #pragma unroll
-                        for (int q = 0; q < 4; ++q) v[q] = __ldcg(reinterpret_cast<const float4*>(pp + wofs + (e * 4 + q) * 128));
+                        for (int q = 0; q < 4; ++q)
+                            v[q] = row_valid ? __ldcg(reinterpret_cast<const float4*>(pp + wofs + (e * 4 + q) * 128)) : make_float4(0.f, 0.f, 0.f, 0.f);
                     };
-                    auto load_ml = [&](const float* pp) { return __ldcg(reinterpret_cast<const float2*>(pp + mlofs)); };
+                    auto load_ml = [&](const float* pp) { return row_valid ? __ldcg(reinterpret_cast<const float2*>(pp + mlofs)) : make_float2(-INFINITY, 0.f); };
                     auto weight = [](float m, float mx) { return m == -INFINITY ? 0.f : ex2(m - mx); };
                     bool last = __shfl_sync(CB_FULL, arrived, 0) == (uint32_t)(np - 1);
                     if (!last) {
@@ -514,11 +550,13 @@ __global__ void __launch_bounds__(kThreads, 1) cb_chunk_tc_kernel(const CbChunkP
                         for (int e = 0; e < npc; ++e) {
                             float o[16];
                             load_o(o, c0 + 16 * e);
+                            if (row_valid) {                  // (a single token's unit has G rows of 128)
 #pragma unroll
-                            for (int q = 0; q < 4; ++q)
-                                *reinterpret_cast<float4*>(own + wofs + (e * 4 + q) * 128) = make_float4(o[q * 4], o[q * 4 + 1], o[q * 4 + 2], o[q * 4 + 3]);
+                                for (int q = 0; q < 4; ++q)
+                                    *reinterpret_cast<float4*>(own + wofs + (e * 4 + q) * 128) = make_float4(o[q * 4], o[q * 4 + 1], o[q * 4 + 2], o[q * 4 + 3]);
+                            }
                         }
-                        *reinterpret_cast<float2*>(own + mlofs) = make_float2(x_m, x_l);
+                        if (row_valid) *reinterpret_cast<float2*>(own + mlofs) = make_float2(x_m, x_l);
                         __syncwarp();
                         if (lane == 0) arrived = atom_add_acq_rel(ticket, 1u);   // releases the whole warp's stores
                         last = __shfl_sync(CB_FULL, arrived, 0) == (uint32_t)(np - 1);
@@ -550,12 +588,20 @@ __global__ void __launch_bounds__(kThreads, 1) cb_chunk_tc_kernel(const CbChunkP
                                 for (int q = 0; q < 4; ++q) v[q] = vn[q];
                             }
                         } else {
-                            for (int k = 0; k < np; ++k) {
-                                const float* pp = part_of(k);
-                                const float2 ml = pp == own ? make_float2(x_m, x_l) : load_ml(pp);
-                                const float mn = fmaxf(mx, ml.x);
-                                sum = fmaf(weight(ml.x, mn), ml.y, sum * weight(mx, mn));
-                                mx = mn;
+                            // Many parts: two at a time are fetched, with their references, before either is used (one after the other, with what
+                            // CTA 5 of 6 left at batch 1, the last to come spent 14 k cycles here).
+                            auto part2 = [&](int k, const float* pp, float2* ml) { *ml = k >= np ? make_float2(-INFINITY, 0.f) : (pp == own ? make_float2(x_m, x_l) : load_ml(pp)); };
+#pragma unroll 1
+                            for (int k = 0; k < np; k += 4) {
+                                float2 ml[4];
+#pragma unroll
+                                for (int t = 0; t < 4; ++t) part2(k + t, part_of(min(k + t, np - 1)), &ml[t]);
+#pragma unroll
+                                for (int t = 0; t < 4; ++t) {
+                                    const float mn = fmaxf(mx, ml[t].x);
+                                    sum = fmaf(weight(ml[t].x, mn), ml[t].y, sum * weight(mx, mn));
+                                    mx = mn;
+                                }
                             }
                             const float inv = sum > 0.f ? 1.0f / sum : 0.f;
 #pragma unroll 1
@@ -564,20 +610,23 @@ __global__ void __launch_bounds__(kThreads, 1) cb_chunk_tc_kernel(const CbChunkP
 #pragma unroll
                                 for (int k = 0; k < 16; ++k) acc[k] = 0.f;
 #pragma unroll 1
-                                for (int k = 0; k < np; ++k) {
-                                    const float* pp = part_of(k);
-                                    float4 v[4];
-                                    float mk = x_m;
-                                    if (pp == own) {
-                                        load_o(reinterpret_cast<float*>(v), c0 + 16 * e);
-                                    } else {
-                                        load_part(v, pp, e);
-                                        mk = load_ml(pp).x;
-                                    }
-                                    const float w = weight(mk, mx);
-                                    const float* vf = reinterpret_cast<const float*>(v);
+                                for (int k = 0; k < np; k += 2) {
+                                    const float* const pp[2] = {part_of(k), part_of(min(k + 1, np - 1))};
+                                    float4 v[2][4];
+                                    float2 ml[2];
 #pragma unroll
-                                    for (int q = 0; q < 16; ++q) acc[q] = fmaf(w, vf[q], acc[q]);
+                                    for (int t = 0; t < 2; ++t) {
+                                        part2(k + t, pp[t], &ml[t]);
+                                        if (pp[t] == own) load_o(reinterpret_cast<float*>(v[t]), c0 + 16 * e);
+                                        else load_part(v[t], pp[t], e);
+                                    }
+#pragma unroll
+                                    for (int t = 0; t < 2; ++t) {
+                                        const float w = weight(ml[t].x, mx);
+                                        const float* vf = reinterpret_cast<const float*>(v[t]);
+#pragma unroll
+                                        for (int q = 0; q < 16; ++q) acc[q] = fmaf(w, vf[q], acc[q]);
+                                    }
                                 }
                                 store_out(acc, c0 + 16 * e, inv);
                             }
@@ -674,7 +723,7 @@ cb_status launch(const CbChunkParams& p, const ChunkMaps& maps, cudaStream_t st,
             if (known) g_smem_set[D == 128][device] = true;
         }
     }
-    CB_CUDA(cb_launch_pdl(cb_chunk_tc_kernel<D>, dim3(p.nc), dim3(kThreads), Cfg<D>::SMEM, st, p, maps));
+    CB_CUDA(cb_launch_pdl(cb_chunk_tc_kernel<D>, dim3(p.cs > 0 ? p.B * p.Hkv * p.cs : p.nc), dim3(kThreads), Cfg<D>::SMEM, st, p, maps));
     cb_count_launch(1);
     return CB_OK;
 }
@@ -692,6 +741,7 @@ cb_status cb_chunk_launch_tensor(cb_ctx* ctx, const CbChunkParams& given, cudaSt
     w.D = p.D;
     cb_attn_weights(w);
     p.w1 = w.w1; p.w2 = w.w2; p.d1 = w.d1; p.d2 = w.d2;
+    p.cs = p.one ? cb_chunk_pick_share((long long)p.B * p.Hkv, ((long long)p.max_keys + CB_KT - 1) / CB_KT, p.nc) : 0;
     p.part = ctx->d_attn_part; p.part_ticket = ctx->d_attn_ticket; p.part_turn = ctx->d_attn_turn;
     ChunkMaps maps;
     if (!encode_pool(&maps.k, p.k_pool, p) || !encode_pool(&maps.v, p.v_pool, p) || !encode_queries(&maps.q, p)) return CB_ERR_CUDA;

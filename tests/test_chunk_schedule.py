@@ -25,9 +25,26 @@ int main() {
                 if (got != other) { printf("lanes differ\n"); return 1; }
                 printf("%d ", got);
             }
+        } else if (what == 3) {                               // few units, many CTAs each
+            CbChunkParams p = {};
+            if (scanf("%d %d %d %d %d %d", &p.B, &p.G, &p.Hkv, &p.D, &p.nc, &p.max_keys) != 6) return 1;
+            std::vector<int> q(p.B + 1), c(p.B);
+            for (int& x : q) if (scanf("%d", &x) != 1) return 1;
+            for (int& x : c) if (scanf("%d", &x) != 1) return 1;
+            p.q_start = q.data(); p.ctx_len = c.data(); p.n_rows = p.max_chunk = q[p.B];
+            p.NPT = CB_MT / p.G; p.one = 1;
+            p.cs = cb_chunk_pick_share((long long)p.B * p.Hkv, (p.max_keys + 127) / 128, p.nc);
+            printf("%d ", p.cs);
+            for (int k = 0; p.cs && k < p.B * p.Hkv * p.cs; ++k) {
+                CbChunkUnit u;
+                CbChunkShape s;
+                int np = 0;
+                if (cb_chunk_share(p, k, &u, &s, &np)) printf("%d %d %d %d %d %d %d ", k, u.b, u.kh, u.t0, u.t1, s.tiles(0), np);
+            }
         } else if (what == 1) {
-            long long n, a, b;
-            if (scanf("%lld %lld %lld", &n, &a, &b) != 3) return 1;
+            long long n;
+            int a, b;
+            if (scanf("%lld %d %d", &n, &a, &b) != 3) return 1;
             printf("%lld ", cb_floor_sum(n, a, b));
         } else {
             CbChunkParams p = {};
@@ -44,19 +61,20 @@ int main() {
             int error = 0;
             for (int k = 0; k < p.nc; ++k) {
                 CbChunkWalker wk = {};
-                long long tot = 0;
+                CbChunkCuts cuts;
                 warp([&](int lane) {
                     CbChunkWalker x;
+                    CbChunkCuts t;
                     int err = 0;
-                    const long long t = cb_chunk_range(p, k, lane, &x, &err);
+                    cb_chunk_range(p, k, lane, &x, &t, &err);
                     if (err) error = err;
-                    if (lane == 7) { wk = x; tot = t; }
+                    if (lane == 7) { wk = x; cuts = t; }
                 });
                 CbChunkUnit u;
                 while (wk.next(p, &u)) {
                     const CbChunkShape& s = wk.s;
-                    const int tiles = s.tiles(u.rg), wt = s.wt(u.rg), cf = cb_cta_of(tot, p.nc, u.first);
-                    const int np = tot >= (long long)p.nc * wt ? cb_cta_of(tot, p.nc, u.first + (long long)(tiles - 1) * wt) - cf + 1 : tiles;
+                    const int tiles = s.tiles(u.rg), wt = s.wt(u.rg), cf = cuts.of(u.first);
+                    const int np = cuts.total >= (long long)p.nc * wt ? cuts.of(u.first + (long long)(tiles - 1) * wt) - cf + 1 : tiles;
                     printf("%d %d %d %d %d %d %d %d %d %d %d %d ", k, u.b, u.kh, u.rg, u.t0, u.t1, tiles, s.two_rows(u.rg) ? 2 : 1, s.row0, s.end(u.rg), cf, np);
                 }
             }
@@ -135,7 +153,7 @@ def _plain(G, hkv, D, nc, max_chunk, q, ctx):
     (1, 32, 128, [1], [4095]), (4, 8, 128, [1] * 64, list(range(120, 8200, 128))), (4, 4, 64, [0, 509, 1, 64, 0, 200], [3, 0, 5000, 640, 9, 0]),
     (8, 8, 128, [8192], [0]), (7, 4, 128, [1000, 3, 18, 19, 36, 37], [77, 0, 5, 250, 1, 128]), (5, 1, 64, [2000, 1], [31, 9000]), (16, 3, 128, [40, 8, 9], [0, 1, 2]),
     (3, 2, 64, [0, 0, 0], [1, 2, 3]), (1, 1, 128, [1], [0]), (2, 2, 128, [300] * 3, [0, 128, 500]), (1, 40, 64, [129, 128, 127, 1], [0, 0, 0, 0]),
-    (4, 1, 128, [1] * 100, [5] * 100),
+    (4, 1, 128, [1] * 100, [5] * 100), (6, 2, 128, [900, 0, 5000], [200, 7, 60]), (16, 1, 64, [2500, 3], [150000, 50]), (3, 4, 128, [1] * 33 + [4000] + [0] * 40 + [2], [9] * 75),
 ])
 def test_who_works_on_what(shim, G, hkv, D, new, ctx):
     q = np.concatenate([[0], np.cumsum(new)]).tolist()
@@ -161,3 +179,26 @@ def test_sequences_that_are_left_out(shim):
         units, error = shim(text).split("\n")[:2]
         got = {int(x[1]) for x in np.array(units.split(), np.int64).reshape(-1, 12)}
         assert int(error) == code and got == {0, 1, 2} - set(np.atleast_1d(left).tolist())
+
+
+@pytest.mark.parametrize("B,G,hkv,new,ctx", [(1, 1, 32, [1], [4095]), (1, 8, 8, [1], [32000]), (3, 4, 2, [1, 0, 7], [5, 10, 4000]), (1, 1, 1, [1], [0]), (2, 16, 1, [8, 3], [0, 127]),
+                                             (9, 4, 8, [1] * 9, [100] * 9), (1, 1, 148, [1], [9000]), (5, 1, 40, [1] * 5, [1000] * 5)])
+def test_few_units_shared_by_many(shim, B, G, hkv, new, ctx):
+    """Every tile of every unit has one CTA, the CTAs of a unit are neighbours from the first on, and none is without tiles among them."""
+    q = np.concatenate([[0], np.cumsum(new)])
+    keys = max(n + c for n, c in zip(new, ctx))
+    for nc in (148, 160):
+        x = [int(y) for y in shim("3 %d %d %d 128 %d %d %s %s\n" % (B, G, hkv, nc, keys, " ".join(map(str, q)), " ".join(map(str, ctx)))).split()]
+        cs, rows = x[0], np.array(x[1:], np.int64).reshape(-1, 7)
+        assert 0 <= cs <= 32 and cs * B * hkv <= nc
+        if cs == 0:
+            assert B * hkv > 40                                   # many units already
+            continue
+        for b in range(B):
+            for kh in range(hkv):
+                mine = rows[(rows[:, 1] == b) & (rows[:, 2] == kh)]
+                tiles = -(-(new[b] + ctx[b]) // 128) if new[b] else 0
+                np_ = min(cs, tiles)
+                assert mine[:, 0].tolist() == list(range((b * hkv + kh) * cs, (b * hkv + kh) * cs + np_))
+                assert sum((list(range(t0, t1)) for t0, t1 in mine[:, 3:5]), []) == list(range(tiles))
+                assert (mine[:, 4] > mine[:, 3]).all() and (mine[:, 5] == tiles).all() and (mine[:, 6] == np_).all()

@@ -82,6 +82,29 @@ def test_many_sequences():
     _compare(out, lse, q, c, 64 ** -0.5)
 
 
+@pytest.mark.parametrize("hq,hkv,d", [(1, 1, 128), (8, 8, 64), (32, 32, 128), (16, 2, 128), (64, 8, 64), (148, 148, 64)])
+def test_single_tokens_of_small_batches_and_then_a_large_launch(hq, hkv, d):
+    """Units shared by up to 32 CTAs, from one key to many tiles each; launches of few CTAs between launches of all (what is counted for the CTAs of
+    one may not reach the next)."""
+    c2 = Paged([90, 1, 33], [700, 2000, 5], hkv, d, seed=4)
+    q2 = _q(int(c2.q_start[-1]), hq, d, c2.g)
+    for new, ctx in (([1], [0]), ([1], [127]), ([1], [128]), ([1], [1300]), ([1], [5000]), ([1, 1], [300, 3]), ([1, 0, 1], [1000, 5, 129])):
+        cb = context(batch=len(new), n_q_heads=hq, n_kv_heads=hkv, head_dim=d)
+        c = Paged(new, ctx, hkv, d, seed=2)
+        q = _q(int(c.q_start[-1]), hq, d, c.g)
+        for _ in range(2):
+            out, lse, st = _run(c, q, cb=cb)
+            assert st == 0
+            _compare(out, lse, q, c, d ** -0.5)
+        if len(new) == 3:
+            for _ in range(3):
+                out, lse, st = _run(c2, q2, cb=cb)
+                assert st == 0
+                _compare(out, lse, q2, c2, d ** -0.5)
+                out, lse, st = _run(c, q, cb=cb)
+                _compare(out, lse, q, c, d ** -0.5)
+
+
 @pytest.mark.parametrize("d", [64, 128])
 def test_long_chunk_on_a_long_context(d):
     c = Paged([1500, 1, 2100], [6000, 9000, 0], 2, d)

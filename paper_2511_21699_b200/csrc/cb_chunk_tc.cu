@@ -519,7 +519,21 @@ __global__ void __launch_bounds__(kThreads, 1) cb_chunk_tc_kernel(const CbChunkP
                 auto store_lse = [&](float mx, float sum) {
                     if (row_valid && c0 == 0 && p.lse) p.lse[at_row] = (mx + log2f(sum)) * 0.6931471805599453f;
                 };
-                if (whole) {
+                if (!whole && p.cs > 0) {
+                    // left in memory by rows, for all threads of the last CTA to put together (below)
+                    float* const own = p.part + (size_t)cta * (CB_MT * (D + 4));
+#pragma unroll 1
+                    for (int e = 0; e < npc; ++e) {
+                        float o[16];
+                        load_o(o, c0 + 16 * e);
+                        if (row_valid) {
+#pragma unroll
+                            for (int q = 0; q < 4; ++q)
+                                *reinterpret_cast<float4*>(own + row * D + c0 + 16 * e + q * 4) = make_float4(o[q * 4], o[q * 4 + 1], o[q * 4 + 2], o[q * 4 + 3]);
+                        }
+                    }
+                    if (row_valid && c0 == 0) *reinterpret_cast<float2*>(own + CB_MT * D + row * 2) = make_float2(x_m, x_l);
+                } else if (whole) {
                     const float inv = x_l > 0.f ? 1.0f / x_l : 0.f;
 #pragma unroll 1
                     for (int e = 0; e < npc; ++e) {
@@ -634,6 +648,56 @@ __global__ void __launch_bounds__(kThreads, 1) cb_chunk_tc_kernel(const CbChunkP
                         store_lse(mx, sum);
                     }
                 }
+            }
+            if (!whole && p.cs > 0) {
+                // The CTA's only unit, shared: all its rows are in memory (row sums' barrier, next phase), one thread counts the CTA in, and
+                // the threads of the last CTA to come put the parts together, an output quad each, with all parts' loads under way at once.
+                // Nobody waits for another CTA.  (A warp's columns by that warp, part after part, took the last CTA 13 k cycles at batch 1.)
+                mbar_arrive(bar_sums);
+                if (!(ok = mbar_wait(bar_sums, 1, s_abort, p.status))) break;
+                volatile int* const s_last = reinterpret_cast<volatile int*>(sgen + C::OFF_X);
+                if (sw == 0 && lane == 0) {
+                    __threadfence();
+                    *s_last = atom_add_acq_rel(p.part_ticket + u->ticket, 1u) == (uint32_t)(np - 1);
+                    __threadfence();
+                }
+                mbar_arrive(bar_ofree(0));                    // (nobody waits there for the accumulator of an only unit)
+                if (!(ok = mbar_wait(bar_ofree(0), 0, s_abort, p.status))) break;
+                if (*s_last) {
+                    const float* const parts = p.part + (size_t)u->cf * (CB_MT * (D + 4));
+                    const int quads = u->n * p.G * (D / 4);
+                    for (int k = sw * 32 + lane; k < quads; k += 512) {
+                        const int r = k / (D / 4), c = k % (D / 4) * 4, tk = token_of(r);
+                        float mx = -INFINITY, sum = 0.f;
+                        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+                        for (int j0 = 0; j0 < np; j0 += 4) {
+                            float2 ml[4];
+                            float4 v[4];
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                const float* pp = parts + (size_t)min(j0 + j, np - 1) * (CB_MT * (D + 4));
+                                ml[j] = __ldcg(reinterpret_cast<const float2*>(pp + CB_MT * D + r * 2));
+                                v[j] = __ldcg(reinterpret_cast<const float4*>(pp + r * D + c));
+                            }
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                if (j0 + j >= np) break;
+                                const float mn = fmaxf(mx, ml[j].x);
+                                const float wo = mx == -INFINITY ? 0.f : ex2(mx - mn), wp = ml[j].x == -INFINITY ? 0.f : ex2(ml[j].x - mn);
+                                mx = mn;
+                                sum = fmaf(wp, ml[j].y, wo * sum);
+                                acc.x = fmaf(wp, v[j].x, wo * acc.x); acc.y = fmaf(wp, v[j].y, wo * acc.y);
+                                acc.z = fmaf(wp, v[j].z, wo * acc.z); acc.w = fmaf(wp, v[j].w, wo * acc.w);
+                            }
+                        }
+                        const float inv = sum > 0.f ? 1.0f / sum : 0.f;
+                        const size_t at = (size_t)(u->row0 + tk) * p.Hq + u->kh * p.G + r - tk * p.G;
+                        *reinterpret_cast<uint2*>(p.out + at * D + c) = make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
+                        if (c == 0 && p.lse) p.lse[at] = (mx + log2f(sum)) * 0.6931471805599453f;
+                    }
+                }
+                break;
             }
             tc_fence_before();
             if (two) mbar_arrive_n(bar_ofree(l), 2u);         // 512 arrivals per unit either way

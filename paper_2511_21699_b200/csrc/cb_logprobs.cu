@@ -5,17 +5,65 @@
 // (x - M) - log s, the entropy log s - t / s (two terms that are not negative, so nothing cancels).
 //
 // The alternatives need no second pass over the row.  Elements are ordered by value, equal ones by falling id (a 64-bit key).  Every
-// thread knows its largest element; the K-th largest of these is a bound that at least K elements reach, and only the K threads above it
-// can hold any that do.  So those K threads' elements, some 1/13 of a row for K = 20, are looked at once more (they are in L2), what reaches
-// the bound is listed, usually little more than K elements, and the list is ranked by counting.
+// thread knows its largest element, and 32 groups of threads each theirs; at least K elements reach the K-th largest of those 32, and only the
+// few threads whose own largest does (some 30 for K = 20) can hold any.  Their elements are looked at once more (they are in L2), what reaches the
+// bound is listed, little more than K elements as a rule, and the list is ranked by counting.  (Ranking the 256 threads' keys, and reading
+// their largest elements again to find the ids, made this part 12 k cycles long beside the 11 k of a row of 32 k bf16 logits.)
+//
+// A row is one CTA's, or, where that leaves SMs idle, a cluster's, whose CTAs take equal parts of it and hand their sums and their K best
+// to the first one through distributed shared memory.
 #include <math.h>
 
 #include "cb_common.cuh"
 
 namespace {
 
-constexpr int kThreads = 256, kUnroll = 4, kWarps = kThreads / 32;
+constexpr int kThreads = 256, kWarps = kThreads / 32;         // (512 threads a row: 5% faster for some shapes, 50% slower for others)
+constexpr int kUnroll = 4;                                    // 16-byte pieces of a thread at a time
+constexpr int kStep = kThreads * kUnroll;                     // and of the CTA
+constexpr int kGroup = kThreads / 32;                         // threads of one of 32 groups
 constexpr int kCand = 1024;                                   // elements listed; more than that are taken one after the other
+
+__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+// The same place in another CTA of the cluster, and loads from there.
+__device__ __forceinline__ uint32_t cluster_addr(uint32_t local, uint32_t rank) {
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(local), "r"(rank));
+    return r;
+}
+__device__ __forceinline__ float ld_cluster_f(uint32_t a) {
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(a) : "memory");
+    return v;
+}
+__device__ __forceinline__ unsigned long long ld_cluster_u64(uint32_t a) {
+    unsigned long long v;
+    asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(a) : "memory");
+    return v;
+}
+
+// Two fp32 values in one 64-bit register pair, for the packed arithmetic of sm_100.
+__device__ __forceinline__ uint64_t f2_pack(float lo, float hi) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ void f2_unpack(uint64_t v, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
+__device__ __forceinline__ uint64_t f2_fma(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ uint64_t f2_add(uint64_t a, uint64_t b) {
+    uint64_t d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ uint64_t f2_mul(uint64_t a, uint64_t b) {
+    uint64_t d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
 
 struct LogprobParams {
     const void* logits;
@@ -24,6 +72,7 @@ struct LogprobParams {
     float *logprobs, *entropy, *top_logprobs;
     int32_t* top_ids;
     int n_rows, n_out, V, K, T, Dmax;
+    int cs;                                                   // CTAs per row
     uint32_t* status;
 };
 
@@ -96,15 +145,70 @@ __device__ __forceinline__ void unpack(const uint4& u, float* x) {
     }
 }
 
+template <bool BF16>
+struct Block { uint4 u[kUnroll]; };                           // what a thread holds of a step
+template <bool BF16>
+__device__ __forceinline__ void load_block(Block<BF16>& b, const Row<BF16>& r, int k0, int end) {
+    const uint32_t none = BF16 ? 0xFF80FF80u : 0xFF800000u;   // -inf
+#pragma unroll
+    for (int q = 0; q < kUnroll; ++q) b.u[q] = k0 + q * kThreads < end ? r.piece(k0 + q * kThreads) : make_uint4(none, none, none, none);
+}
+// Largest and smallest element; NaN is passed over.
+template <bool BF16>
+__device__ __forceinline__ void extremes(const Block<BF16>& b, float& hi, float& lo) {
+    const uint32_t* w = reinterpret_cast<const uint32_t*>(b.u);
+    if constexpr (BF16) {
+        __nv_bfloat162 h = *reinterpret_cast<const __nv_bfloat162*>(w), l = h;
+#pragma unroll
+        for (int i = 1; i < 4 * kUnroll; ++i) {
+            const __nv_bfloat162 x = *reinterpret_cast<const __nv_bfloat162*>(w + i);
+            h = __hmax2(h, x);
+            l = __hmin2(l, x);
+        }
+        hi = fmaxf(__low2float(h), __high2float(h));
+        lo = fminf(__low2float(l), __high2float(l));
+    } else {
+        hi = -INFINITY; lo = INFINITY;
+#pragma unroll
+        for (int i = 0; i < 4 * kUnroll; i += 2) {
+            const float x = __uint_as_float(w[i]), y = __uint_as_float(w[i + 1]);
+            asm("max.f32 %0, %0, %1, %2;" : "+f"(hi) : "f"(x), "f"(y));
+            asm("min.f32 %0, %0, %1, %2;" : "+f"(lo) : "f"(x), "f"(y));
+        }
+    }
+}
+// Adds a block to s and t on reference ref.  FORBIDDEN: there may be -inf among the elements, whose e d = 0 * -inf must not be NaN.
+template <bool BF16, bool FORBIDDEN>
+__device__ __forceinline__ void add_block(const Block<BF16>& b, float ref, uint64_t& s2, uint64_t& t2) {
+    const uint64_t neg = f2_pack(-ref, -ref), l2e = f2_pack(kLog2e, kLog2e);
+    const uint32_t* w = reinterpret_cast<const uint32_t*>(b.u);
+#pragma unroll
+    for (int i = 0; i < (BF16 ? 4 : 2) * kUnroll; ++i) {
+        uint64_t d = BF16 ? f2_pack(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xFFFF0000u))
+                          : f2_pack(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
+        d = f2_add(d, neg);
+        float a, c;
+        if (FORBIDDEN) {
+            f2_unpack(d, a, c);
+            d = f2_pack(max_keep_nan(a, -3e38f), max_keep_nan(c, -3e38f));
+        }
+        f2_unpack(f2_mul(d, l2e), a, c);
+        const uint64_t e = f2_pack(ex2_approx(a), ex2_approx(c));
+        s2 = f2_add(s2, e);
+        t2 = f2_fma(e, d, t2);
+    }
+}
+
 template <bool BF16, bool TOP>
-__global__ void __launch_bounds__(kThreads) cb_logprobs_kernel(const LogprobParams p) {
+__global__ void __launch_bounds__(kThreads, 4) cb_logprobs_kernel(const LogprobParams p) {
     CB_PDL_ENTRY();
     constexpr int E = Row<BF16>::E;
-    __shared__ Stat s_stat[kWarps];
-    __shared__ unsigned long long s_key[TOP ? kThreads : 1], s_cand[TOP ? kCand : 1], s_bound, s_best[kWarps];
-    __shared__ int s_list[CB_MAX_TOP], s_lists, s_count;
+    __shared__ Stat s_stat[kWarps], s_all;
+    __shared__ unsigned long long s_key[32], s_cand[TOP ? kCand : 1], s_best[kWarps], s_top[TOP ? CB_MAX_TOP : 1];
+    __shared__ int s_list[TOP ? kThreads : 1], s_lists, s_count;
+    __shared__ uint4 s_max[TOP ? kUnroll : 1][TOP ? kThreads : 1];          // every thread's step with its largest element
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int i = blockIdx.x;
+    const int i = blockIdx.x / p.cs, part = blockIdx.x - i * p.cs;          // the row's output, and which part of the row is this CTA's
     int row = i, tok = p.tokens ? p.tokens[i] : 0;
     bool pad = tok < 0, bad = tok >= p.V;
     if (p.accept_nodes) {
@@ -117,7 +221,8 @@ __global__ void __launch_bounds__(kThreads) cb_logprobs_kernel(const LogprobPara
         pad = pad || row < 0;
         bad = bad || row >= p.n_rows;
     }
-    if (pad || bad) {
+    if (pad || bad) {                                         // the whole cluster
+        if (part > 0) return;
         if (bad && !pad && tid == 0) atomicCAS(p.status, 0u, (uint32_t)CB_ERR_INVALID_ARG);
         if (tid == 0) {
             if (p.logprobs && p.tokens) p.logprobs[i] = 0.f;
@@ -127,42 +232,50 @@ __global__ void __launch_bounds__(kThreads) cb_logprobs_kernel(const LogprobPara
         return;
     }
     const Row<BF16> r(p.logits, (long long)row * p.row_stride, p.V);
-    const float x_tok = p.tokens && p.logprobs ? r.at(tok) : 0.f;
+    const float x_tok = part == 0 && p.tokens && p.logprobs ? r.at(tok) : 0.f;
+    const int per = (r.pieces + p.cs - 1) / p.cs, begin = min(part * per, r.pieces), end = min(begin + per, r.pieces);
 
-    Stat a = {-INFINITY, 0.f, 0.f};
-    int best = 0;                                             // step at which the thread's largest element of a piece came
-    for (int k0 = tid, step = 0; k0 < r.pieces; k0 += kThreads * kUnroll, ++step) {
-        uint4 u[kUnroll];
-        const uint32_t none = BF16 ? 0xFF80FF80u : 0xFF800000u;
-#pragma unroll
-        for (int q = 0; q < kUnroll; ++q) u[q] = k0 + q * kThreads < r.pieces ? r.piece(k0 + q * kThreads) : make_uint4(none, none, none, none);
-        float m = -INFINITY;
-#pragma unroll
-        for (int q = 0; q < kUnroll; ++q) {
-            float x[E];
-            unpack<BF16>(u[q], x);
-#pragma unroll
-            for (int j = 0; j < E; ++j) m = fmaxf(m, x[j]);
-        }
-        if (m > a.m) {
-            best = step;
-            shift(a, m);
-        }
-        const float ref = a.m == -INFINITY ? 0.f : a.m;
-#pragma unroll
-        for (int q = 0; q < kUnroll; ++q) {
-            float x[E];
-            unpack<BF16>(u[q], x);
-#pragma unroll
-            for (int j = 0; j < E; ++j) {
-                const float d = max_keep_nan(x[j] - ref, -3e38f), e = ex2_approx(d * kLog2e);     // e = 0 times -inf would be NaN
-                a.s += e;
-                a.t = fmaf(e, d, a.t);
+    float ref = -INFINITY;                                    // the thread's running maximum
+    uint64_t s2 = 0, t2 = 0;                                  // two sums each
+    int best = 0;                                             // step at which the maximum came
+    Block<BF16> cur, next;                                    // (three steps in shared memory, by bulk copies, were no faster than one ahead in registers)
+    load_block(cur, r, begin + tid, end);
+    for (int k0 = begin + tid, step = 0; k0 < end; k0 += kStep, ++step) {
+        load_block(next, r, k0 + kStep, end);
+        float hi, lo;
+        extremes(cur, hi, lo);
+        if (hi > ref) {                                       // -inf: nothing yet (or NaN, which stays)
+            if (ref > -INFINITY) {
+                const float d = ref - hi, w = ex2_approx(d * kLog2e);
+                float s0, s1, t0, t1;
+                f2_unpack(s2, s0, s1);
+                f2_unpack(t2, t0, t1);
+                t2 = w > 0.f ? f2_pack(w * fmaf(s0, d, t0), w * fmaf(s1, d, t1)) : 0;      // (s d may be infinite where w is 0)
+                s2 = f2_pack(s0 * w, s1 * w);
             }
+            ref = hi;
+            if constexpr (TOP) {
+                best = step;
+#pragma unroll
+                for (int q = 0; q < kUnroll; ++q) s_max[q][tid] = cur.u[q];
+            }
+        } else if (TOP && step == 0) {                        // nothing but -inf
+#pragma unroll
+            for (int q = 0; q < kUnroll; ++q) s_max[q][tid] = cur.u[q];
         }
+        const float base = ref == -INFINITY ? 0.f : ref;
+        if (lo == -INFINITY) add_block<BF16, true>(cur, base, s2, t2);
+        else add_block<BF16, false>(cur, base, s2, t2);
+        cur = next;
     }
-    const float top_m = a.m;
-    const int odds = r.head + r.tail;                         // at most 14 elements outside the pieces
+    Stat a;
+    {
+        float s0, s1, t0, t1;
+        f2_unpack(s2, s0, s1);
+        f2_unpack(t2, t0, t1);
+        a = {ref, s0 + s1, t0 + t1};
+    }
+    const int odds = part == 0 ? r.head + r.tail : 0;         // at most 14 elements outside the pieces: the first CTA's
     const int my_odd = tid < odds ? r.odd(tid) : -1;
     const float x_odd = my_odd >= 0 ? r.at(my_odd) : -INFINITY;
     if (my_odd >= 0) {
@@ -175,69 +288,89 @@ __global__ void __launch_bounds__(kThreads) cb_logprobs_kernel(const LogprobPara
     if (lane == 0) s_stat[warp] = a;
     unsigned long long mine = 0;
     if constexpr (TOP) {
-        // this thread's largest element, the lowest id among equal ones
-        const int k0 = tid + best * kThreads * kUnroll;
-        for (int q = 0; q < kUnroll && mine == 0; ++q) {
-            const int k = k0 + q * kThreads;
-            if (k >= r.pieces) break;
+        // this thread's largest element, the lowest id among equal ones, and its group's
+        const int k0 = begin + tid + best * kStep;
+#pragma unroll
+        for (int q = kUnroll - 1; q >= 0; --q) {
+            if (k0 + q * kThreads >= end) continue;
             float x[E];
-            unpack<BF16>(r.piece(k), x);
+            unpack<BF16>(s_max[q][tid], x);
+            int at = -1;
 #pragma unroll
             for (int j = E - 1; j >= 0; --j)
-                if (x[j] == top_m) mine = key_of(x[j], r.id(k, j));
+                if (x[j] == ref) at = j;
+            if (at >= 0) mine = key_of(ref, r.id(k0 + q * kThreads, at));
         }
-        s_key[tid] = mine;
-        if (tid == 0) { s_bound = 0; s_count = 0; s_lists = 0; }
+        unsigned long long group = mine;
+#pragma unroll
+        for (int o = 1; o < kGroup; o <<= 1) group = max(group, __shfl_xor_sync(CB_FULL, group, o));
+        if (lane % kGroup == 0) s_key[tid / kGroup] = group;
+        if (tid == 0) { s_count = 0; s_lists = 0; }
     }
     __syncthreads();
-    a = s_stat[0];
+    if (warp == 0) {                                          // the CTA's sums; only this warp writes any result
+        a = s_stat[lane % kWarps];
 #pragma unroll
-    for (int w = 1; w < kWarps; ++w) a = join(a, s_stat[w]);
-    const float log_s = a.m == -INFINITY ? NAN : logf(a.s);
-    if (tid == 0) {
-        if (p.tokens && p.logprobs) p.logprobs[i] = (x_tok - a.m) - log_s;
-        if (p.entropy) p.entropy[i] = log_s - a.t / a.s;
+        for (int o = kWarps / 2; o > 0; o >>= 1) a = join(a, {__shfl_xor_sync(CB_FULL, a.m, o), __shfl_xor_sync(CB_FULL, a.s, o), __shfl_xor_sync(CB_FULL, a.t, o)});
+        if (lane == 0) s_all = a;
     }
     if constexpr (TOP) {
-        // the K threads with the largest elements, and the K-th of those
+        // the bound, in every warp, and the threads that reach it
+        const unsigned long long key = s_key[lane];
         int rank = 0;
-        for (int k = 0; k < kThreads; ++k) rank += s_key[k] > mine;
-        if (mine != 0 && rank < p.K) {
-            s_list[rank] = tid;
-            if (rank == p.K - 1) s_bound = mine;
-            atomicAdd(&s_lists, 1);
-        }
+#pragma unroll
+        for (int o = 0; o < 32; ++o) rank += s_key[o] > key;
+        const uint32_t who = __ballot_sync(CB_FULL, key != 0 && rank == p.K - 1);
+        const unsigned long long bound = who ? __shfl_sync(CB_FULL, key, __ffs(who) - 1) : 0;    // 0: fewer than K groups have any
+        const float least = bound ? value_of(bound) : -INFINITY;
+        if (mine != 0 && mine >= bound) s_list[atomicAdd(&s_lists, 1)] = tid;
         __syncthreads();
-        const unsigned long long bound = s_bound;
         const int lists = s_lists;
         auto list = [&](unsigned long long k) {
             if (k < bound) return;
             const int at = atomicAdd(&s_count, 1);
             if (at < kCand) s_cand[at] = k;
         };
-        for (int l = warp; l < lists; l += kWarps)
-            for (int k = s_list[l] + lane * kThreads; k < r.pieces; k += 32 * kThreads) {
-                float x[E];
-                unpack<BF16>(r.piece(k), x);
+        // all their pieces dealt to the threads, four loads at a time
+        const int rounds = (end - begin + kThreads - 1) / kThreads, all = lists * rounds;
+        const float inv_rounds = 1.0f / (float)max(rounds, 1);
+        auto div_rounds = [&](int w) {                        // w / rounds; the product is off by one at most
+            int l = (int)((float)w * inv_rounds);
+            if (l * rounds > w) --l;
+            else if ((l + 1) * rounds <= w) ++l;
+            return l;
+        };
+        for (int w0 = tid; w0 < all; w0 += 4 * kThreads) {
+            int at[4];
+            uint4 u[4];
 #pragma unroll
-                for (int j = 0; j < E; ++j) list(key_of(x[j], r.id(k, j)));
+            for (int q = 0; q < 4; ++q) {
+                const int w = w0 + q * kThreads, l = div_rounds(w);
+                at[q] = w < all ? begin + s_list[l] + (w - l * rounds) * kThreads : end;
+                if (at[q] < end) u[q] = r.piece(at[q]);
             }
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                if (at[q] >= end) continue;
+                float x[E], hi = -INFINITY;
+                unpack<BF16>(u[q], x);
+#pragma unroll
+                for (int j = 0; j < E; ++j) hi = fmaxf(hi, x[j]);
+                if (hi < least) continue;                     // most pieces
+#pragma unroll
+                for (int j = 0; j < E; ++j) list(key_of(x[j], r.id(at[q], j)));
+            }
+        }
         const unsigned long long odd_key = my_odd >= 0 ? key_of(x_odd, my_odd) : 0;
         if (my_odd >= 0) list(odd_key);
         __syncthreads();
         const int count = s_count, found = min(count, p.K);
-        int32_t* const ids = p.top_ids + (size_t)i * p.K;
-        float* const lps = p.top_logprobs + (size_t)i * p.K;
-        auto put = [&](int at, unsigned long long k) {
-            ids[at] = id_of(k);
-            lps[at] = (value_of(k) - a.m) - log_s;
-        };
         if (count <= kCand) {
             for (int c = tid; c < count; c += kThreads) {
                 const unsigned long long k = s_cand[c];
                 int at = 0;
                 for (int o = 0; o < count; ++o) at += s_cand[o] > k;
-                if (at < p.K) put(at, k);
+                if (at < p.K) s_top[at] = k;
             }
         } else {
             // a few threads' elements make up much of what is large (a sorted row, say): one after the other
@@ -245,7 +378,7 @@ __global__ void __launch_bounds__(kThreads) cb_logprobs_kernel(const LogprobPara
             for (int at = 0; at < found; ++at) {
                 unsigned long long k1 = odd_key < last ? odd_key : 0;
                 for (int l = warp; l < lists; l += kWarps)
-                    for (int k = s_list[l] + lane * kThreads; k < r.pieces; k += 32 * kThreads) {
+                    for (int k = begin + s_list[l] + lane * kThreads; k < end; k += 32 * kThreads) {
                         float x[E];
                         unpack<BF16>(r.piece(k), x);
 #pragma unroll
@@ -260,19 +393,92 @@ __global__ void __launch_bounds__(kThreads) cb_logprobs_kernel(const LogprobPara
                 __syncthreads();
                 for (int w = 0; w < kWarps; ++w) k1 = max(k1, s_best[w]);
                 last = k1;
-                if (tid == 0) put(at, k1);
+                if (tid == 0) s_top[at] = k1;
                 __syncthreads();
             }
         }
-        if (tid >= found && tid < p.K) { ids[tid] = -1; lps[tid] = -INFINITY; }
+        if (tid >= found && tid < p.K) s_top[tid] = 0;
     }
+    if (p.cs > 1) {
+        // The first CTA reads what the others have; they stay until it has.
+        asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+        if (part == 0) {
+            if (warp == 0) {
+                const uint32_t o = cluster_addr(smem_u32(&s_all), (uint32_t)(lane % p.cs));      // a power of two
+                a = {ld_cluster_f(o), ld_cluster_f(o + 4), ld_cluster_f(o + 8)};
+                for (int d = p.cs / 2; d > 0; d >>= 1) a = join(a, {__shfl_xor_sync(CB_FULL, a.m, d), __shfl_xor_sync(CB_FULL, a.s, d), __shfl_xor_sync(CB_FULL, a.t, d)});
+            }
+            if constexpr (TOP) {
+                const int n = p.cs * p.K;                     // at most 8 lists of 32
+                for (int k = tid; k < n; k += kThreads) s_cand[k] = ld_cluster_u64(cluster_addr(smem_u32(&s_top[k % p.K]), (uint32_t)(k / p.K)));
+                __syncthreads();
+                unsigned long long k = 0;
+                int rank = 0;
+                if (tid < n) {
+                    k = s_cand[tid];
+                    for (int o = 0; o < n; ++o) rank += s_cand[o] > k;
+                }
+                __syncthreads();
+                if (tid < p.K) s_top[tid] = 0;
+                __syncthreads();
+                if (k != 0 && rank < p.K) s_top[rank] = k;
+            }
+        }
+        asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+        if (part > 0) {
+            asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+            return;
+        }
+    }
+    const float log_s = a.m == -INFINITY ? NAN : logf(a.s);
+    if (tid == 0) {
+        if (p.tokens && p.logprobs) p.logprobs[i] = (x_tok - a.m) - log_s;
+        if (p.entropy) p.entropy[i] = log_s - a.t / a.s;
+    }
+    if constexpr (TOP) {
+        __syncthreads();
+        if (tid < p.K) {
+            const unsigned long long k = s_top[tid];
+            p.top_ids[(size_t)i * p.K + tid] = k == 0 ? -1 : id_of(k);
+            p.top_logprobs[(size_t)i * p.K + tid] = k == 0 ? -INFINITY : (value_of(k) - a.m) - log_s;
+        }
+    }
+    if (p.cs > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
-cb_status launch_logprobs(const cb_logprobs_args& a, const LogprobParams& p, cudaStream_t st) {
+// CTAs per row.  A cluster costs a launch some 0.3 us and every row the hand-over; it pays where rows alone leave SMs without work, and, with
+// up to four CTAs an SM, where a row is so long that its CTA ends well after the rest.  Measured, us with 1, 2, 4, 8 CTAs a row:
+//   9 rows of 128 k fp32 10.6, 7.6, 5.6, 4.6;  40 of 128 k bf16 12.4, 8.9, 7.0, 7.8;  75 of 50 k fp32 10.4, 8.3, 7.9, 9.7
+//   150 of 128 k bf16 15.1, 16.6, 14.8, 16.9;  300 of 128 k bf16 27.6, 21.8, 23.3, 28.4;  300 of 50 k fp32 14.7, 18.4, 20.1, 24.7
+//   150 of 128 k fp32 with 20 alternatives 30.6, 27.7, 31.7, 38.3;  9 of 32 k bf16 with five 6.4, 7.1, 6.8, 6.7;  600 of 128 k 34.8, 35.0, 39.9, 52.8
+int pick_cluster(long long rows, int V, int K, int num_sms) {
+    int cs = 1;
+    if (V < 48000) return cs;
+    while (cs < 8) {
+        const long long ctas = rows * cs * 2, each = V / (cs * 2);
+        const bool idle = ctas * 10 <= 11ll * num_sms, room = ctas * 10 <= 42ll * num_sms;
+        if (!(idle ? each >= 12000 : room && each >= (K ? 64000 : 32000))) break;
+        cs *= 2;
+    }
+    return cs;
+}
+
+cb_status launch_logprobs(const cb_logprobs_args& a, LogprobParams p, int num_sms, cudaStream_t st) {
     const bool f32 = a.logits_dtype == CB_DTYPE_F32;
+    p.cs = pick_cluster(p.n_out, p.V, p.K, num_sms);
+    if ((long long)p.n_out * p.cs > 0x7FFFFFFFll) return CB_ERR_UNSUPPORTED;
     auto kernel = p.K ? (f32 ? cb_logprobs_kernel<false, true> : cb_logprobs_kernel<true, true>)
                       : (f32 ? cb_logprobs_kernel<false, false> : cb_logprobs_kernel<true, false>);
-    CB_CUDA(cb_launch_pdl(kernel, dim3((unsigned)p.n_out), dim3(kThreads), 0, st, p));
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(p.n_out * p.cs)); cfg.blockDim = dim3(kThreads); cfg.stream = st;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = (unsigned)p.cs; at[1].val.clusterDim.y = 1; at[1].val.clusterDim.z = 1;
+    cfg.attrs = at; cfg.numAttrs = p.cs > 1 ? 2 : 1;
+    CB_CUDA(cudaLaunchKernelEx(&cfg, kernel, p));
     cb_count_launch(1);
     return CB_OK;
 }
@@ -302,7 +508,7 @@ extern "C" cb_status cb_logprobs(cb_ctx* ctx, const cb_logprobs_args* a, void* s
     if (a->n_out == 0) return CB_OK;
     LogprobParams p = params_of(ctx, *a);
     p.rows = a->rows; p.tokens = a->tokens; p.n_rows = a->n_rows; p.n_out = a->n_out;
-    return launch_logprobs(*a, p, (cudaStream_t)stream);
+    return launch_logprobs(*a, p, ctx->num_sms, (cudaStream_t)stream);
 }
 
 extern "C" cb_status cb_accept_logprobs(cb_ctx* ctx, const int32_t* accept_nodes, const int32_t* out_tokens, const cb_logprobs_args* a, void* stream) {
@@ -311,5 +517,5 @@ extern "C" cb_status cb_accept_logprobs(cb_ctx* ctx, const int32_t* accept_nodes
     LogprobParams p = params_of(ctx, *a);
     p.accept_nodes = accept_nodes; p.tokens = out_tokens;
     p.n_out = ctx->cfg.batch * (ctx->cfg.max_depth + 1);
-    return launch_logprobs(*a, p, (cudaStream_t)stream);
+    return launch_logprobs(*a, p, ctx->num_sms, (cudaStream_t)stream);
 }

@@ -29,7 +29,8 @@ def _logits(n, V, dtype, seed, spread=3.0):
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("n,V,top", [(1, 32000, 5), (3, 1, 1), (7, 5, 5), (5, 31, 20), (4, 257, 32), (33, 5003, 0), (9, 50257, 20), (2, 128256, 32), (300, 4099, 3),
-                                     (1, 151936, 0), (1000, 2048, 1), (37, 8191, 12)])
+                                     (1, 151936, 0), (1000, 2048, 1), (37, 8191, 12), (40, 128256, 32), (70, 50257, 6), (150, 130001, 0), (149, 128256, 20),
+                                     (18, 100003, 31)])
 def test_rows(n, V, top, dtype):
     cb = context(vocab=V)
     x, tok = _logits(n, V, dtype, n + V)
@@ -39,8 +40,12 @@ def test_rows(n, V, top, dtype):
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_rows_at_odd_places(dtype):
-    """A view whose rows start at every offset within 16 bytes, read through a list of rows that names some twice."""
-    V, n = 5003, 19
+    """A view whose rows start at every offset within 16 bytes, read through a list of rows that names some twice; rows of one CTA and of several."""
+    for V, n in ((5003, 19), (60001, 11)):
+        _odd_places(V, n, dtype)
+
+
+def _odd_places(V, n, dtype):
     cb = context(vocab=V)
     store, _ = _logits(n, V + 6, dtype, 5)
     x = store[:, 1:V + 1]
@@ -51,8 +56,13 @@ def test_rows_at_odd_places(dtype):
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_order_of_the_alternatives(dtype):
-    """Ties go to the lowest id, wherever the large elements lie: constant rows, sorted ones, all of them in one thread's elements, -0 and 0."""
-    V = 20000
+    """Ties go to the lowest id, wherever the large elements lie: constant rows, sorted ones, all of them in one thread's elements, -0 and 0.
+    The longer rows are a cluster's: ties across its CTAs too."""
+    for V in (20000, 80000):
+        _order(V, dtype)
+
+
+def _order(V, dtype):
     cb = context(vocab=V)
     ramp = torch.arange(V, device="cuda", dtype=torch.float32)
     one = torch.zeros(V, device="cuda")

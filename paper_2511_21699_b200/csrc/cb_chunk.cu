@@ -19,7 +19,8 @@ __global__ void __launch_bounds__(32 * kWarps) cb_chunk_cc_kernel(const CbChunkP
     const long long item = (long long)blockIdx.x * kWarps + (threadIdx.x >> 5);
     if (item >= (long long)p.n_rows * p.Hq) return;
     const int row = (int)(item / p.Hq), h = (int)(item % p.Hq), kh = h / p.G;
-    const int b = cb_find_sequence(p.q_start, p.B, row, lane);
+    int q0, q1, ctx;
+    const int b = cb_find_sequence(p.q_start, p.B, row, lane, p.ctx_len, &q0, &q1, &ctx);
     if (b < 0) return;
     const CbChunkSeq s = cb_chunk_seq(p, b);
     if (s.error && lane == 0) atomicCAS(p.status, 0u, (uint32_t)s.error);

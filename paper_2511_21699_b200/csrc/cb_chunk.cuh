@@ -2,8 +2,9 @@
 #pragma once
 #include "cb_common.cuh"
 
-// The last b < B with q_start[b] <= r, by the whole warp, 32 probes at a time; -1 if there is none.
-__device__ __forceinline__ int cb_find_sequence(const int32_t* q_start, int B, int r, int lane) {
+// The last b < B with q_start[b] <= r, by the whole warp, 32 probes at a time; -1 if there is none.  With it come its rows' bounds and its cached
+// length, which the last round's lanes fetch beside their probes.
+__device__ __forceinline__ int cb_find_sequence(const int32_t* q_start, int B, int r, int lane, const int32_t* ctx_len, int* q0, int* q1, int* ctx) {
     int lo = 0, n = B;                                        // it is in [lo, lo + n), or there is none
     while (n > 32) {
         const int step = (n + 31) / 32, at = lo + lane * step;
@@ -13,8 +14,13 @@ __device__ __forceinline__ int cb_find_sequence(const int32_t* q_start, int B, i
         n = min(step, n - l * step);
         lo += l * step;
     }
-    const uint32_t hit = __ballot_sync(CB_FULL, lane < n && q_start[lo + lane] <= r);
-    return hit == 0u ? -1 : lo + 31 - __clz(hit);
+    int start = 0, end = 0, c = 0;
+    if (lane < n) { start = q_start[lo + lane]; end = q_start[lo + lane + 1]; c = ctx_len[lo + lane]; }
+    const uint32_t hit = __ballot_sync(CB_FULL, lane < n && start <= r);
+    if (hit == 0u) return -1;
+    const int l = 31 - __clz(hit);
+    *q0 = __shfl_sync(CB_FULL, start, l); *q1 = __shfl_sync(CB_FULL, end, l); *ctx = __shfl_sync(CB_FULL, c, l);
+    return lo + l;
 }
 
 // What attention of packed chunks is given.

@@ -4,7 +4,7 @@
 // Each element is read once and written once, so HBM bounds it; the arithmetic is some ten instructions a pair.  D / 16 lanes share a
 // head and a lane holds two pieces of 8 elements that are rotated with one another (i with i + R / 2) or each in itself (neighbouring
 // pairs), so a rotation needs no exchange between lanes and the norm's sum two or three shuffles.  A warp takes 4 (D = 128) or 8
-// (D = 64) heads of one row; which sequence the row belongs to is found while its elements are on their way.
+// (D = 64) heads of one row, or two or four times as many; which sequence the row belongs to is found while its elements are on their way.
 #include "cb_chunk.cuh"
 
 namespace {
@@ -38,46 +38,54 @@ __device__ __forceinline__ uint4 pack8(const float* x) {
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-template <int D, bool TREE>
+template <int D, bool TREE, int U>
 __global__ void __launch_bounds__(32 * kRopeWarps) cb_rope_kernel(const RopeParams p) {
     CB_PDL_ENTRY();
-    constexpr int LPH = D / 16, HPW = 32 / LPH;
+    constexpr int LPH = D / 16, HPW = 32 / LPH;               // lanes per head, heads that a warp holds side by side
     const int lane = threadIdx.x & 31, sub = lane % LPH;
-    const long long item = (long long)blockIdx.x * kRopeWarps + (threadIdx.x >> 5);
-    const long long row64 = item / p.parts;
-    if (row64 >= p.n_rows) return;                            // a whole warp
-    const int row = (int)row64, slot = (int)(item % p.parts) * HPW + lane / LPH;
-    // which head this is: the row's queries, then its keys, then its values
-    const bool is_q = slot < p.Hq, is_k = !is_q && slot < p.Hq + p.Hkv, is_v = !is_q && !is_k && slot < p.Hq + 2 * p.Hkv;
-    const int h = is_q ? slot : (is_k ? slot - p.Hq : slot - p.Hq - p.Hkv);
+    const uint32_t item = blockIdx.x * kRopeWarps + (threadIdx.x >> 5);
+    const uint32_t urow = item / (uint32_t)p.parts;
+    if (urow >= (uint32_t)p.n_rows) return;                   // a whole warp
+    const int row = (int)urow, slot0 = (int)(item - urow * (uint32_t)p.parts) * (U * HPW) + lane / LPH;
     const int R = p.rope ? p.R : 0;
     const bool turned = sub < R / 16;                         // both pieces are, or neither
     int ca = 2 * sub, cb = 2 * sub + 1;
     if (turned && !p.interleaved) { ca = sub; cb = sub + R / 16; }   // (the lanes behind these hold what lies behind R)
-    uint4 ua = make_uint4(0, 0, 0, 0), ub = ua;
-    const __nv_bfloat16* src = is_q ? p.q + row64 * p.q_stride : (is_k ? p.k + row64 * p.k_stride : p.v + row64 * p.v_stride);
-    if (is_q || is_k || is_v) {
-        ua = *reinterpret_cast<const uint4*>(src + (size_t)h * D + ca * 8);
-        ub = *reinterpret_cast<const uint4*>(src + (size_t)h * D + cb * 8);
+    // A row's heads in one count: its queries, then its keys, then its values.
+    auto is_q = [&](int u) { return slot0 + u * HPW < p.Hq; };
+    auto is_qk = [&](int u) { return slot0 + u * HPW < p.Hq + p.Hkv; };
+    auto is_any = [&](int u) { return slot0 + u * HPW < p.Hq + 2 * p.Hkv; };
+    uint4 ua[U], ub[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int slot = slot0 + u * HPW;
+        const __nv_bfloat16* src = is_q(u) ? p.q + row * p.q_stride + slot * D
+                                           : (is_qk(u) ? p.k + row * p.k_stride + (slot - p.Hq) * D : p.v + row * p.v_stride + (slot - p.Hq - p.Hkv) * D);
+        ua[u] = ub[u] = make_uint4(0, 0, 0, 0);
+        if (is_any(u)) {
+            ua[u] = *reinterpret_cast<const uint4*>(src + ca * 8);
+            ub[u] = *reinterpret_cast<const uint4*>(src + cb * 8);
+        }
     }
     // the row's position, and its place in the cache; the same in all lanes
     long long pos = 0;
-    size_t kv_row = row64;
+    size_t kv_row = (size_t)row;
     bool dead = false;
     if constexpr (TREE) {
-        const int b = row / p.T, i = row % p.T;
+        const int b = row / p.T, i = row - b * p.T;
+        const int ctx = p.ctx_len[b], depth = p.depth[row];
         dead = i >= p.n_nodes[b];
         if (!dead) {
-            pos = (long long)p.ctx_len[b] + p.depth[row];
+            pos = (long long)ctx + depth;
             if (pos < 0 || (p.rope && pos >= p.rope_len)) {
                 dead = true;
                 if (lane == 0) atomicCAS(p.status, 0u, (uint32_t)CB_ERR_INVALID_ARG);
             }
         }
     } else {
-        const int b = cb_find_sequence(p.q_start, p.B, row, lane);
+        int q0, q1, ctx;
+        const int b = cb_find_sequence(p.q_start, p.B, row, lane, p.ctx_len, &q0, &q1, &ctx);
         if (b < 0) return;
-        const int q0 = p.q_start[b], q1 = p.q_start[b + 1], ctx = p.ctx_len[b];
         if (row < q0 || row >= q1) return;                    // behind the last sequence
         const bool full = (long long)ctx + q1 - q0 > (long long)p.max_pages * p.P;
         pos = (long long)ctx + row - q0;
@@ -85,63 +93,73 @@ __global__ void __launch_bounds__(32 * kRopeWarps) cb_rope_kernel(const RopePara
             if (lane == 0) atomicCAS(p.status, 0u, (uint32_t)(ctx >= 0 && full ? CB_ERR_KV_FULL : CB_ERR_INVALID_ARG));
             return;
         }
-        const int page = p.block_table[(size_t)b * p.max_pages + pos / p.P];
+        const uint32_t at = (uint32_t)pos / (uint32_t)p.P;    // (a position is below 2^31: it fits the pages, or the sum would be full)
+        const int page = p.block_table[(size_t)b * p.max_pages + at];
         if (page < 0 || page >= p.num_pages) {
             if (lane == 0) atomicCAS(p.status, 0u, (uint32_t)CB_ERR_INVALID_ARG);
             return;
         }
-        kv_row = (size_t)page * p.P + pos % p.P;
+        kv_row = (size_t)page * p.P + ((uint32_t)pos - at * (uint32_t)p.P);
     }
-    if (dead) {
-        ua = ub = make_uint4(0, 0, 0, 0);
-    } else {
-        const __nv_bfloat16* w = is_q ? p.q_norm : p.k_norm;
-        float a[8], b[8];
-        unpack8(ua, a);
-        unpack8(ub, b);
-        float ss = 0.f;
+    float c[8], s[8];                                         // the same for every head of the row
+    if (turned && !dead) {
+        const float4* rc = reinterpret_cast<const float4*>(p.rope + pos * R + 8 * sub);
+        const float4* rs = reinterpret_cast<const float4*>(p.rope + pos * R + R / 2 + 8 * sub);
+        *reinterpret_cast<float4*>(c) = rc[0]; *reinterpret_cast<float4*>(c + 4) = rc[1];
+        *reinterpret_cast<float4*>(s) = rs[0]; *reinterpret_cast<float4*>(s + 4) = rs[1];
+    }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) ss = fmaf(a[i], a[i], fmaf(b[i], b[i], ss));
+    for (int u = 0; u < U; ++u) {
+        const int slot = slot0 + u * HPW;
+        if (dead) {
+            ua[u] = ub[u] = make_uint4(0, 0, 0, 0);
+        } else {
+            const __nv_bfloat16* w = is_q(u) ? p.q_norm : p.k_norm;
+            float a[8], b[8];
+            unpack8(ua[u], a);
+            unpack8(ub[u], b);
+            if (p.q_norm || p.k_norm) {                       // all lanes: the sum is by shuffles
+                float ss = 0.f;
 #pragma unroll
-        for (int o = 1; o < LPH; o <<= 1) ss += __shfl_xor_sync(CB_FULL, ss, o);
-        if (is_q || is_k) {
-            if (w) {
-                const float inv = rsqrtf(ss * (1.0f / D) + p.eps);
-                float wa[8], wb[8];
-                unpack8(*reinterpret_cast<const uint4*>(w + ca * 8), wa);
-                unpack8(*reinterpret_cast<const uint4*>(w + cb * 8), wb);
+                for (int i = 0; i < 8; ++i) ss = fmaf(a[i], a[i], fmaf(b[i], b[i], ss));
 #pragma unroll
-                for (int i = 0; i < 8; ++i) { a[i] *= inv * wa[i]; b[i] *= inv * wb[i]; }
-            }
-            if (turned) {
-                float c[8], s[8];
-                const float4* rc = reinterpret_cast<const float4*>(p.rope + pos * R + 8 * sub);
-                const float4* rs = reinterpret_cast<const float4*>(p.rope + pos * R + R / 2 + 8 * sub);
-                *reinterpret_cast<float4*>(c) = rc[0]; *reinterpret_cast<float4*>(c + 4) = rc[1];
-                *reinterpret_cast<float4*>(s) = rs[0]; *reinterpret_cast<float4*>(s + 4) = rs[1];
-                if (p.interleaved) {
+                for (int o = 1; o < LPH; o <<= 1) ss += __shfl_xor_sync(CB_FULL, ss, o);
+                if (is_qk(u) && w) {
+                    const float inv = rsqrtf(ss * (1.0f / D) + p.eps);
+                    float wa[8], wb[8];
+                    unpack8(*reinterpret_cast<const uint4*>(w + ca * 8), wa);
+                    unpack8(*reinterpret_cast<const uint4*>(w + cb * 8), wb);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float a0 = a[2 * i], a1 = a[2 * i + 1], b0 = b[2 * i], b1 = b[2 * i + 1];
-                        a[2 * i] = a0 * c[i] - a1 * s[i]; a[2 * i + 1] = a1 * c[i] + a0 * s[i];
-                        b[2 * i] = b0 * c[4 + i] - b1 * s[4 + i]; b[2 * i + 1] = b1 * c[4 + i] + b0 * s[4 + i];
-                    }
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const float x = a[i], y = b[i];
-                        a[i] = x * c[i] - y * s[i];
-                        b[i] = y * c[i] + x * s[i];
-                    }
+                    for (int i = 0; i < 8; ++i) { a[i] *= inv * wa[i]; b[i] *= inv * wb[i]; }
                 }
             }
-            if (w || turned) { ua = pack8(a); ub = pack8(b); }
+            if (is_qk(u)) {
+                if (turned) {
+                    if (p.interleaved) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const float a0 = a[2 * i], a1 = a[2 * i + 1], b0 = b[2 * i], b1 = b[2 * i + 1];
+                            a[2 * i] = a0 * c[i] - a1 * s[i]; a[2 * i + 1] = a1 * c[i] + a0 * s[i];
+                            b[2 * i] = b0 * c[4 + i] - b1 * s[4 + i]; b[2 * i + 1] = b1 * c[4 + i] + b0 * s[4 + i];
+                        }
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const float x = a[i], y = b[i];
+                            a[i] = x * c[i] - y * s[i];
+                            b[i] = y * c[i] + x * s[i];
+                        }
+                    }
+                }
+                if (w || turned) { ua[u] = pack8(a); ub[u] = pack8(b); }
+            }
         }
-    }
-    if (is_q || is_k || is_v) {
-        __nv_bfloat16* dst = is_q ? p.q_out + (size_t)row64 * p.Hq * D : (is_k ? p.k_out : p.v_out) + kv_row * p.Hkv * D;
-        *reinterpret_cast<uint4*>(dst + (size_t)h * D + ca * 8) = ua;
-        *reinterpret_cast<uint4*>(dst + (size_t)h * D + cb * 8) = ub;
+        if (is_any(u)) {
+            __nv_bfloat16* dst = is_q(u) ? p.q_out + (size_t)row * p.Hq * D + slot * D
+                                         : (is_qk(u) ? p.k_out + kv_row * p.Hkv * D + (slot - p.Hq) * D : p.v_out + kv_row * p.Hkv * D + (slot - p.Hq - p.Hkv) * D);
+            *reinterpret_cast<uint4*>(dst + ca * 8) = ua[u];
+            *reinterpret_cast<uint4*>(dst + cb * 8) = ub[u];
+        }
     }
 }
 
@@ -167,16 +185,26 @@ RopeParams params_of(cb_ctx* ctx, const cb_qkv_rows& r) {
     return p;
 }
 
-template <bool TREE>
-cb_status launch_rope(RopeParams p, int D, cudaStream_t st) {
-    const int per_warp = 32 / (D / 16);
+template <bool TREE, int U>
+cb_status launch_rope_of(RopeParams p, int D, cudaStream_t st) {
+    const int per_warp = U * 32 / (D / 16);
     p.parts = (p.Hq + 2 * p.Hkv + per_warp - 1) / per_warp;
     const long long blocks = ((long long)p.n_rows * p.parts + kRopeWarps - 1) / kRopeWarps;
-    if (blocks > 0x7FFFFFFFll) return CB_ERR_UNSUPPORTED;
-    auto kernel = D == 128 ? cb_rope_kernel<128, TREE> : cb_rope_kernel<64, TREE>;
+    if (blocks * kRopeWarps > 0x7FFFFFFFll) return CB_ERR_UNSUPPORTED;
+    auto kernel = D == 128 ? cb_rope_kernel<128, TREE, U> : cb_rope_kernel<64, TREE, U>;
     CB_CUDA(cb_launch_pdl(kernel, dim3((unsigned)blocks), dim3(32 * kRopeWarps), 0, st, p));
     cb_count_launch(1);
     return CB_OK;
+}
+// Groups of heads per warp: one where warps are few, since a call then takes what one of them takes; more where there are plenty, since what
+// belongs to the row (its sequence, position, page, angles) is found once for all of them and their loads are under way together.  us with 1, 2, 4:
+// 8,192 rows of 64/8 heads 87.8, 75.2, 68.1; 16,384 tree rows of them 158, 125, 123; 4,096 of 32/8 26.4, 23.5, 22.4; 2,048 tree rows of 32/8 13.7, 11.3, 13.3.
+template <bool TREE>
+cb_status launch_rope(const RopeParams& p, int D, cudaStream_t st) {
+    const int per_warp = 32 / (D / 16);
+    const long long groups = (long long)p.n_rows * ((p.Hq + 2 * p.Hkv + per_warp - 1) / per_warp);
+    if (groups >= 40000) return launch_rope_of<TREE, 4>(p, D, st);
+    return groups >= 8000 ? launch_rope_of<TREE, 2>(p, D, st) : launch_rope_of<TREE, 1>(p, D, st);
 }
 
 }  // namespace

@@ -18,10 +18,18 @@ int main() {
             int B, n;
             if (scanf("%d %d", &B, &n) != 2) return 1;
             std::vector<int> q(B + 1);
+            std::vector<int> ctx(B);
             for (int& x : q) if (scanf("%d", &x) != 1) return 1;
+            for (int b = 0; b < B; ++b) ctx[b] = 7 * b + 1;
             for (int r = 0; r < n; ++r) {
                 int got = -2, other = -2;
-                warp([&](int lane) { const int b = cb_find_sequence(q.data(), B, r, lane); if (lane == 0) got = b; if (lane == 31) other = b; });
+                warp([&](int lane) {
+                    int q0 = 0, q1 = 0, c = 0;
+                    const int b = cb_find_sequence(q.data(), B, r, lane, ctx.data(), &q0, &q1, &c);
+                    if (b >= 0 && (q0 != q[b] || q1 != q[b + 1] || c != ctx[b])) got = other = -3;
+                    else if (lane == 0) got = b;
+                    else if (lane == 31) other = b;
+                });
                 if (got != other) { printf("lanes differ\n"); return 1; }
                 printf("%d ", got);
             }

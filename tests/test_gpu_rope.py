@@ -32,6 +32,10 @@ def _check(got, x, w, eps, table, pos, inter, what):
     (16, 4, 64, 48, True, True, [16, 16, 16], [0, 16, 8]),
     (3, 3, 64, 0, True, False, [4, 1], [9, 0]),
     (7, 7, 128, 0, False, False, [6], [3]),
+    (64, 8, 128, 128, True, False, [700, 1, 800], [5, 100, 0]),   # two groups of heads a warp, not all of them there
+    (64, 8, 128, 64, True, True, [2100], [3]),                    # four
+    (21, 7, 64, 64, True, False, [9000], [0]),
+    (40, 40, 64, 32, False, False, [3000], [1000]),
 ])
 @pytest.mark.parametrize("packed", [True, False])
 def test_append(hq, hkv, d, rot, norm, inter, new, ctx, packed):
@@ -41,7 +45,7 @@ def test_append(hq, hkv, d, rot, norm, inter, new, ctx, packed):
     q, k, v = qkv[:, :hq], qkv[:, hq:hq + hkv], qkv[:, hq + hkv:]
     if not packed:
         q, k, v = q.contiguous(), k.contiguous(), v.contiguous()
-    table = rope_table(4200, rot) if rot else None
+    table = rope_table(max(4200, max(new) + max(ctx)), rot) if rot else None
     wq, wk = _norms(d, c.g, norm)
     cb = context(batch=len(new), n_q_heads=hq, n_kv_heads=hkv, head_dim=d)
     kp, vp = c.k.clone(), c.v.clone()
@@ -113,7 +117,7 @@ def test_append_leaves_sequences_alone_that_do_not_fit():
 
 
 @pytest.mark.parametrize("hq,hkv,d,T,rot,norm,inter", [(32, 8, 128, 64, 128, True, False), (16, 4, 64, 61, 32, False, True), (8, 8, 64, 1, 64, True, True),
-                                                       (5, 1, 128, 128, 96, True, False)])
+                                                       (5, 1, 128, 128, 96, True, False), (64, 8, 128, 128, 128, True, False), (200, 200, 128, 128, 128, True, True)])
 def test_tree(hq, hkv, d, T, rot, norm, inter):
     B = 5
     g = torch.Generator(device="cuda").manual_seed(T)

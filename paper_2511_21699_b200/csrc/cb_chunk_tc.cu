@@ -43,8 +43,8 @@ struct Cfg {
     static constexpr uint32_t OFF_Q = 0;                      // two row tiles
     static constexpr uint32_t OFF_RING = 2 * Q_BYTES;
     static constexpr uint32_t OFF_BAR = OFF_RING + NSLOT * TILE_BYTES;
-    // slot_full[NSLOT], slot_free[NSLOT], q_full, q_free, s_full[2], p_ready[2], o_done[2], o_done_both, o_free[2], sums, unit_full[kUnitRing]
-    static constexpr int NBAR = 2 * NSLOT + 12 + kUnitRing;
+    // slot_full[NSLOT], slot_free[NSLOT], q_full[2], q_free[2], s_full[2], p_ready[2], o_done[2], o_done_both, o_free[2], sums, unit_full[kUnitRing]
+    static constexpr int NBAR = 2 * NSLOT + 14 + kUnitRing;
     static constexpr uint32_t OFF_UNITS = OFF_BAR + NBAR * 8;
     static constexpr uint32_t OFF_X = (OFF_UNITS + kUnitRing * sizeof(ChunkUnit) + 15) / 16 * 16;   // [2 chains][2][128 rows]
     static constexpr uint32_t OFF_MISC = OFF_X + 2 * 2 * CB_MT * 4;                  // positions of all units, tmem base, abort flag, pair counters
@@ -71,14 +71,16 @@ __global__ void __launch_bounds__(kThreads, 1) cb_chunk_tc_kernel(const CbChunkP
     auto bar_free = [&](uint32_t s) { return bar0 + 8u * (C::NSLOT + s); };
     auto slot_base = [&](uint32_t s) { return sbase + C::OFF_RING + s * C::TILE_BYTES; };
     constexpr uint32_t B1 = 2 * C::NSLOT;
-    const uint32_t bar_qfull = bar0 + 8u * B1, bar_qfree = bar_qfull + 8u;
-    auto bar_sfull = [&](int l) { return bar0 + 8u * (B1 + 2 + l); };
-    auto bar_pready = [&](int l) { return bar0 + 8u * (B1 + 4 + l); };
-    auto bar_odone = [&](int l) { return bar0 + 8u * (B1 + 6 + l); };
-    const uint32_t bar_odone_both = bar0 + 8u * (B1 + 8);
-    auto bar_ofree = [&](int l) { return bar0 + 8u * (B1 + 9 + l); };
-    const uint32_t bar_sums = bar0 + 8u * (B1 + 11);
-    auto bar_ufull = [&](uint32_t k) { return bar0 + 8u * (B1 + 12 + k); };
+    auto bar_qfull = [&](int k) { return bar0 + 8u * (B1 + k); };
+    auto bar_qfree = [&](int k) { return bar0 + 8u * (B1 + 2 + k); };
+    auto bar_sfull = [&](int l) { return bar0 + 8u * (B1 + 4 + l); };
+    auto bar_pready = [&](int l) { return bar0 + 8u * (B1 + 6 + l); };
+    auto bar_odone = [&](int l) { return bar0 + 8u * (B1 + 8 + l); };
+    const uint32_t bar_odone_both = bar0 + 8u * (B1 + 10);
+    auto bar_ofree = [&](int l) { return bar0 + 8u * (B1 + 11 + l); };
+    const uint32_t bar_sums = bar0 + 8u * (B1 + 13);
+    auto bar_ufull = [&](uint32_t k) { return bar0 + 8u * (B1 + 14 + k); };
+    constexpr uint32_t kSoftWarps = 16;                       // a warp arrives once, behind a __syncwarp
     ChunkUnit* s_units = reinterpret_cast<ChunkUnit*>(sgen + C::OFF_UNITS);
     volatile float* s_x = reinterpret_cast<volatile float*>(sgen + C::OFF_X);
     volatile long long* s_tot = reinterpret_cast<volatile long long*>(sgen + C::OFF_MISC);
@@ -95,12 +97,12 @@ __global__ void __launch_bounds__(kThreads, 1) cb_chunk_tc_kernel(const CbChunkP
     } else if (warp == 2) {
         if (lane == 0) {
             for (int s = 0; s < C::NSLOT; ++s) { mbar_init(bar_full(s), 1); mbar_init(bar_free(s), 1); }
-            mbar_init(bar_qfull, 1); mbar_init(bar_qfree, 1);
             for (int l = 0; l < 2; ++l) {
-                mbar_init(bar_sfull(l), 1); mbar_init(bar_pready(l), 256);
-                mbar_init(bar_odone(l), 1); mbar_init(bar_ofree(l), 512);
+                mbar_init(bar_qfull(l), 1); mbar_init(bar_qfree(l), 1);
+                mbar_init(bar_sfull(l), 1); mbar_init(bar_pready(l), kSoftWarps / 2);
+                mbar_init(bar_odone(l), 1); mbar_init(bar_ofree(l), kSoftWarps);
             }
-            mbar_init(bar_odone_both, 1); mbar_init(bar_sums, 512);
+            mbar_init(bar_odone_both, 1); mbar_init(bar_sums, kSoftWarps);
             for (int k = 0; k < kUnitRing; ++k) mbar_init(bar_ufull(k), 1);
             *s_abort = 0;
             asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -160,7 +162,7 @@ __global__ void __launch_bounds__(kThreads, 1) cb_chunk_tc_kernel(const CbChunkP
             if (elect_one()) {
                 constexpr uint32_t idesc_s = make_idesc(128, CB_KT, false);
                 constexpr uint32_t idesc_o = make_idesc(128, D, true);
-                uint32_t uq = 0, c_p[2] = {0u, 0u};
+                uint32_t uq = 0, c_p[2] = {0u, 0u}, c_q1 = 0;     // (every unit has a first query tile, some a second one)
                 while ((ok = mbar_wait(bar_ufull(uq % kUnitRing), (uq / kUnitRing) & 1, s_abort, p.status))) {
                     const volatile ChunkUnit* u = &s_units[uq % kUnitRing];
                     const int nrt = u->nrt;
@@ -169,7 +171,7 @@ __global__ void __launch_bounds__(kThreads, 1) cb_chunk_tc_kernel(const CbChunkP
                     const int nt = u->t1 - u->t0, nev = two ? 2 * nt : nt;
                     const uint32_t seq0 = (uint32_t)u->seq0;
                     const int nt0 = nt - u->skip;             // tiles of the first chain
-                    if (!(ok = mbar_wait(bar_qfull, uq & 1, s_abort, p.status))) break;
+                    if (!(ok = mbar_wait(bar_qfull(0), uq & 1, s_abort, p.status))) break;
                     // Turn e belongs to chain e & 1: the P V of its turn before (key tile iv), then S of this turn's key tile ik.
                     for (int e = 0; e < nev + 2; ++e) {
                         const int l = e & 1, ik = two ? e >> 1 : e, iv = two ? ik - 1 : ik - 2;
@@ -194,12 +196,14 @@ __global__ void __launch_bounds__(kThreads, 1) cb_chunk_tc_kernel(const CbChunkP
                                 if (!(ok = mbar_wait(bar_full(ks), (kseq / ns) & 1, s_abort, p.status))) break;
                                 tc_fence_after();
                             }
+                            if (two && e == 1) {
+                                if (!(ok = mbar_wait(bar_qfull(1), c_q1++ & 1, s_abort, p.status))) break;
+                                tc_fence_after();
+                            }
                             mma_s_grouped_block<D>(tmem + l * 128, desc_lo(sbase + C::OFF_Q + (two ? l : 0) * C::Q_BYTES, 16), desc_lo(slot_base(ks), 16), idesc_s);
                             tc_commit(bar_sfull(l));
-                            if (!two || l == 1) {
-                                tc_commit(bar_free(ks));
-                                if (ik == nt - 1) tc_commit(bar_qfree);
-                            }
+                            if (!two || l == 1) tc_commit(bar_free(ks));
+                            if (ik == mine - 1) tc_commit(bar_qfree(two ? l : 0));
                         }
                     }
                     if (!ok) break;
@@ -226,12 +230,25 @@ __global__ void __launch_bounds__(kThreads, 1) cb_chunk_tc_kernel(const CbChunkP
                 seq += 2 * (x.t1 - x.t0);
                 mbar_arrive(bar_ufull(uq % kUnitRing));
             };
+            // A unit's query tiles, each when the one before it there has been read; the next unit's are asked into L2 as soon as it is known.
+            uint32_t n_q1 = 0;
+            auto query_box = [&](const CbChunkUnit& x, const CbChunkShape& s, int k, int db, bool ahead) {
+                const int c0 = db * 64, c1 = x.kh * p.G, c2 = s.row0 + (2 * x.rg + k) * p.NPT;
+                if (ahead) asm volatile("cp.async.bulk.prefetch.tensor.4d.L2.global.tile [%0, {%1, %2, %3, %4}];" ::"l"(&maps.q), "r"(c0), "r"(c1), "r"(c2), "r"(0) : "memory");
+                else tma_load_4d(sbase + C::OFF_Q + k * C::Q_BYTES + db * (CB_MT * 128), &maps.q, bar_qfull(k), c0, c1, c2, 0);
+            };
             auto load_queries = [&](const CbChunkUnit& x, const CbChunkShape& s) {
                 const int nrt = s.two_rows(x.rg) ? 2 : 1;
-                mbar_expect_tx(bar_qfull, (uint32_t)(nrt * C::DB * RT * 128));
-                for (int k = 0; k < nrt; ++k)
-                    for (int db = 0; db < C::DB; ++db)
-                        tma_load_4d(sbase + C::OFF_Q + k * C::Q_BYTES + db * (CB_MT * 128), &maps.q, bar_qfull, db * 64, x.kh * p.G, s.row0 + (2 * x.rg + k) * p.NPT, 0);
+                if (uq > 0)
+                    for (int k = 0; k < nrt; ++k)
+                        for (int db = 0; db < C::DB; ++db) query_box(x, s, k, db, true);
+                for (int k = 0; k < nrt; ++k) {
+                    const uint32_t before = k == 0 ? uq : n_q1;
+                    if (before > 0 && !(ok = mbar_wait(bar_qfree(k), (before - 1) & 1, s_abort, p.status))) return;
+                    mbar_expect_tx(bar_qfull(k), (uint32_t)(C::DB * RT * 128));
+                    for (int db = 0; db < C::DB; ++db) query_box(x, s, k, db, false);
+                    if (k == 1) ++n_q1;
+                }
             };
             CbChunkUnit x;
             if (p.cs > 0) {
@@ -270,8 +287,8 @@ __global__ void __launch_bounds__(kThreads, 1) cb_chunk_tc_kernel(const CbChunkP
                             u->ticket = ticket_set + cf * 16;
                         }
                         publish(x, s);
-                        if (uq > 0 && !(ok = mbar_wait(bar_qfree, (uq - 1) & 1, s_abort, p.status))) break;
                         load_queries(x, s);
+                        if (!ok) break;
                         ++uq;
                     }
                 }
@@ -319,6 +336,8 @@ __global__ void __launch_bounds__(kThreads, 1) cb_chunk_tc_kernel(const CbChunkP
             const int limit = u->ctx + token + 1;             // keys that this row sees
             const uint32_t ts = tmem + l * 128 + lane_addr, tsh = ts + 64 * hf;
             const uint32_t tm_O = tmem + C::O_COL + l * D + lane_addr;
+            // the tile in whose last page there are slots behind the sequence's last token, for the warp that clears them
+            const int unclean = u->dirty && hf == 0 && wq == 0 && (!two || l == u->skip) ? u->tiles - 1 : -1;
             float m_used = -INFINITY, lsum = 0.f;
             for (int i = tfirst; i < t1; i += step) {
                 if (!(ok = mbar_wait(bar_sfull(l), c_s & 1, s_abort, p.status))) break;
@@ -432,9 +451,8 @@ __global__ void __launch_bounds__(kThreads, 1) cb_chunk_tc_kernel(const CbChunkP
                     lsum += lt;
                     tmem_wait_st();
                 }
-                if (u->dirty && i == u->tiles - 1 && hf == 0 && wq == 0 && (!two || l == u->skip)) {
-                    // The last page goes on behind the sequence's last token: zeros there before any product reads the tile.  With two row
-                    // tiles that is for the chain whose product comes first.
+                if (i == unclean) {
+                    // Zeros there before any product reads the tile; with two row tiles by the chain whose product comes first.
                     const uint32_t vseq = (uint32_t)u->seq0 + 2u * (uint32_t)(i - u->t0) + 1u, vs = vseq % ns;
                     if (!(ok = mbar_wait(bar_full(vs), (vseq / ns) & 1, s_abort, p.status))) break;
                     const int r0 = u->ctx + u->n - i * CB_KT, pieces = u->dirty * (D / 8);
@@ -446,7 +464,8 @@ __global__ void __launch_bounds__(kThreads, 1) cb_chunk_tc_kernel(const CbChunkP
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 }
                 tc_fence_before();
-                mbar_arrive(bar_pready(l));
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar_pready(l));
             }
             if (!ok) break;
             // ---- epilogue of this unit's share
@@ -477,7 +496,8 @@ __global__ void __launch_bounds__(kThreads, 1) cb_chunk_tc_kernel(const CbChunkP
                 const float lrow = lsum + s_x[(l * 2 + 1 - hf) * CB_MT + row];
                 pair_sync(false, 3);
                 s_x[(l * 2 + hf) * CB_MT + row] = hf ? lrow : m_used;
-                mbar_arrive(bar_sums);
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar_sums);
                 if (!(ok = mbar_wait(bar_sums, (c_ob - 1) & 1, s_abort, p.status))) break;
                 const float m0 = s_x[row], l0 = s_x[CB_MT + row], m1 = s_x[2 * CB_MT + row], l1 = s_x[3 * CB_MT + row];
                 x_m = fmaxf(m0, m1);
@@ -653,7 +673,8 @@ __global__ void __launch_bounds__(kThreads, 1) cb_chunk_tc_kernel(const CbChunkP
                 // The CTA's only unit, shared: all its rows are in memory (row sums' barrier, next phase), one thread counts the CTA in, and
                 // the threads of the last CTA to come put the parts together, an output quad each, with all parts' loads under way at once.
                 // Nobody waits for another CTA.  (A warp's columns by that warp, part after part, took the last CTA 13 k cycles at batch 1.)
-                mbar_arrive(bar_sums);
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar_sums);
                 if (!(ok = mbar_wait(bar_sums, 1, s_abort, p.status))) break;
                 volatile int* const s_last = reinterpret_cast<volatile int*>(sgen + C::OFF_X);
                 if (sw == 0 && lane == 0) {
@@ -661,7 +682,7 @@ __global__ void __launch_bounds__(kThreads, 1) cb_chunk_tc_kernel(const CbChunkP
                     *s_last = atom_add_acq_rel(p.part_ticket + u->ticket, 1u) == (uint32_t)(np - 1);
                     __threadfence();
                 }
-                mbar_arrive(bar_ofree(0));                    // (nobody waits there for the accumulator of an only unit)
+                if (lane == 0) mbar_arrive(bar_ofree(0));     // (nobody waits there for the accumulator of an only unit)
                 if (!(ok = mbar_wait(bar_ofree(0), 0, s_abort, p.status))) break;
                 if (*s_last) {
                     const float* const parts = p.part + (size_t)u->cf * (CB_MT * (D + 4));
@@ -700,8 +721,11 @@ __global__ void __launch_bounds__(kThreads, 1) cb_chunk_tc_kernel(const CbChunkP
                 break;
             }
             tc_fence_before();
-            if (two) mbar_arrive_n(bar_ofree(l), 2u);         // 512 arrivals per unit either way
-            else { mbar_arrive(bar_ofree(0)); mbar_arrive(bar_ofree(1)); }
+            __syncwarp();
+            if (lane == 0) {                                  // 16 arrivals per unit either way
+                if (two) mbar_arrive_n(bar_ofree(l), 2u);
+                else { mbar_arrive(bar_ofree(0)); mbar_arrive(bar_ofree(1)); }
+            }
         }
         if (!ok) {
             // The other warp of the pair may have entered a pair barrier that this one will not: answer for it until it has left too.

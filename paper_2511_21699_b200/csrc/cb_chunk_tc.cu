@@ -43,15 +43,20 @@ struct Cfg {
     static constexpr uint32_t OFF_Q = 0;                      // two row tiles
     static constexpr uint32_t OFF_RING = 2 * Q_BYTES;
     static constexpr uint32_t OFF_BAR = OFF_RING + NSLOT * TILE_BYTES;
-    // slot_full[NSLOT], slot_free[NSLOT], q_full[2], q_free[2], s_full[2], p_ready[2], o_done[2], o_done_both, o_free[2], sums, unit_full[kUnitRing]
-    static constexpr int NBAR = 2 * NSLOT + 14 + kUnitRing;
+    // slot_full[NSLOT], slot_free[NSLOT], q_full[2], q_free[2], s_full[3], p_ready[3], pv_done[3], o_done[2], o_done_both, o_free[2], sums, unit_full[kUnitRing]
+    static constexpr int NBAR = 2 * NSLOT + 19 + kUnitRing;
     static constexpr uint32_t OFF_UNITS = OFF_BAR + NBAR * 8;
     static constexpr uint32_t OFF_X = (OFF_UNITS + kUnitRing * sizeof(ChunkUnit) + 15) / 16 * 16;   // [2 chains][2][128 rows]
     static constexpr uint32_t OFF_MISC = OFF_X + 2 * 2 * CB_MT * 4;                  // positions of all units, tmem base, abort flag, pair counters
     static constexpr uint32_t SMEM = OFF_MISC + 16 + 64;
     static_assert(SMEM <= 227 * 1024, "shared memory of one CTA");
     static constexpr int FMA_EXP = (D == 128) ? 8 : 4;        // of so many pairs of exponentials the last is taken by the FMA pipe
-    static constexpr uint32_t O_COL = 256;                    // TMEM columns: S0 at 0, S1 at 128, O0 at 256, O1 at 256 + D
+    // TMEM columns: the S buffers 128 apart from 0, O0 and O1 behind them.  With head_dim 128 a chain has one S buffer, and its next S
+    // follows the product that reads the P over the last one.  With 64 there is room for a third, and the turns of both chains take the three in turn:
+    // the next S of a chain is there before its softmax is done with the one before, and the product comes behind it.
+    static constexpr int NSB = (D == 128) ? 2 : 3;
+    static constexpr uint32_t O_COL = NSB * 128;
+    static_assert(O_COL + 2 * D <= kTmemCols, "tensor memory of an SM");
 };
 
 struct ChunkMaps { CUtensorMap k, v, q; };
@@ -73,13 +78,14 @@ __global__ void __launch_bounds__(kThreads, 1) cb_chunk_tc_kernel(const CbChunkP
     constexpr uint32_t B1 = 2 * C::NSLOT;
     auto bar_qfull = [&](int k) { return bar0 + 8u * (B1 + k); };
     auto bar_qfree = [&](int k) { return bar0 + 8u * (B1 + 2 + k); };
-    auto bar_sfull = [&](int l) { return bar0 + 8u * (B1 + 4 + l); };
-    auto bar_pready = [&](int l) { return bar0 + 8u * (B1 + 6 + l); };
-    auto bar_odone = [&](int l) { return bar0 + 8u * (B1 + 8 + l); };
-    const uint32_t bar_odone_both = bar0 + 8u * (B1 + 10);
-    auto bar_ofree = [&](int l) { return bar0 + 8u * (B1 + 11 + l); };
-    const uint32_t bar_sums = bar0 + 8u * (B1 + 13);
-    auto bar_ufull = [&](uint32_t k) { return bar0 + 8u * (B1 + 14 + k); };
+    auto bar_sfull = [&](int k) { return bar0 + 8u * (B1 + 4 + k); };      // by S buffer, as the next two
+    auto bar_pready = [&](int k) { return bar0 + 8u * (B1 + 7 + k); };
+    auto bar_pvdone = [&](int k) { return bar0 + 8u * (B1 + 10 + k); };    // three buffers only
+    auto bar_odone = [&](int l) { return bar0 + 8u * (B1 + 13 + l); };
+    const uint32_t bar_odone_both = bar0 + 8u * (B1 + 15);
+    auto bar_ofree = [&](int l) { return bar0 + 8u * (B1 + 16 + l); };
+    const uint32_t bar_sums = bar0 + 8u * (B1 + 18);
+    auto bar_ufull = [&](uint32_t k) { return bar0 + 8u * (B1 + 19 + k); };
     constexpr uint32_t kSoftWarps = 16;                       // a warp arrives once, behind a __syncwarp
     ChunkUnit* s_units = reinterpret_cast<ChunkUnit*>(sgen + C::OFF_UNITS);
     volatile float* s_x = reinterpret_cast<volatile float*>(sgen + C::OFF_X);
@@ -99,9 +105,9 @@ __global__ void __launch_bounds__(kThreads, 1) cb_chunk_tc_kernel(const CbChunkP
             for (int s = 0; s < C::NSLOT; ++s) { mbar_init(bar_full(s), 1); mbar_init(bar_free(s), 1); }
             for (int l = 0; l < 2; ++l) {
                 mbar_init(bar_qfull(l), 1); mbar_init(bar_qfree(l), 1);
-                mbar_init(bar_sfull(l), 1); mbar_init(bar_pready(l), kSoftWarps / 2);
                 mbar_init(bar_odone(l), 1); mbar_init(bar_ofree(l), kSoftWarps);
             }
+            for (int k = 0; k < C::NSB; ++k) { mbar_init(bar_sfull(k), 1); mbar_init(bar_pready(k), kSoftWarps / 2); mbar_init(bar_pvdone(k), 1); }
             mbar_init(bar_odone_both, 1); mbar_init(bar_sums, kSoftWarps);
             for (int k = 0; k < kUnitRing; ++k) mbar_init(bar_ufull(k), 1);
             *s_abort = 0;
@@ -162,50 +168,65 @@ __global__ void __launch_bounds__(kThreads, 1) cb_chunk_tc_kernel(const CbChunkP
             if (elect_one()) {
                 constexpr uint32_t idesc_s = make_idesc(128, CB_KT, false);
                 constexpr uint32_t idesc_o = make_idesc(128, D, true);
-                uint32_t uq = 0, c_p[2] = {0u, 0u}, c_q1 = 0;     // (every unit has a first query tile, some a second one)
+                uint32_t uq = 0, turn0 = 0, c_p[2] = {0u, 0u}, c_q1 = 0;     // (every unit has a first query tile, some a second one)
                 while ((ok = mbar_wait(bar_ufull(uq % kUnitRing), (uq / kUnitRing) & 1, s_abort, p.status))) {
                     const volatile ChunkUnit* u = &s_units[uq % kUnitRing];
                     const int nrt = u->nrt;
                     if (nrt == 0) break;
                     const bool two = nrt == 2;
-                    const int nt = u->t1 - u->t0, nev = two ? 2 * nt : nt;
+                    const int nt = u->t1 - u->t0;
                     const uint32_t seq0 = (uint32_t)u->seq0;
                     const int nt0 = nt - u->skip;             // tiles of the first chain
                     if (!(ok = mbar_wait(bar_qfull(0), uq & 1, s_abort, p.status))) break;
-                    // Turn e belongs to chain e & 1: the P V of its turn before (key tile iv), then S of this turn's key tile ik.
-                    for (int e = 0; e < nev + 2; ++e) {
-                        const int l = e & 1, ik = two ? e >> 1 : e, iv = two ? ik - 1 : ik - 2;
-                        const int mine = two && l == 0 ? nt0 : nt;
-                        if (e >= 2 && iv < mine) {
-                            const uint32_t vseq = seq0 + 2u * (uint32_t)iv + 1u, vs = vseq % ns;
-                            if ((!two || l == 0 || iv >= nt0) && !(ok = mbar_wait(bar_full(vs), (vseq / ns) & 1, s_abort, p.status))) break;
-                            // the unit before is done with this chain's accumulator; a chain without a tile of this unit takes its turn
-                            // on the barrier here too
-                            if (e < 4 && uq > 0 && !(ok = mbar_wait(bar_ofree(l), (uq - 1) & 1, s_abort, p.status))) break;
-                            if (nev < 2 && uq > 0 && !(ok = mbar_wait(bar_ofree(1), (uq - 1) & 1, s_abort, p.status))) break;
-                            const uint32_t vdesc = desc_lo(slot_base(vs), 1024), o_at = tmem + C::O_COL + l * D, p_at = tmem + l * 128, parity = c_p[l]++ & 1;
-                            if (!(ok = mbar_wait(bar_pready(l), parity, s_abort, p.status))) break;
-                            tc_fence_after();
-                            mma_pv_halves_block<D>(o_at, p_at, vdesc, idesc_o, e < 4 ? 0u : 1u);
-                            if (!two || l == 1) tc_commit(bar_free(vs));
-                            if (iv >= mine - 1) tc_commit(two ? bar_odone(l) : bar_odone_both);
+                    // Turn e is tile e / 2 for chain e & 1 with two row tiles, else tile e for chain e & 1.  Its S goes out behind the P V of NSB turns before,
+                    // whose buffer it takes.  A tile that the first chain leaves out is a turn of nobody's; with three buffers, which
+                    // go by the count of turns, it is none, and the last turn is the second chain's whatever its number.
+                    const int skip = nt - nt0, turns = two ? 2 * nt - (C::NSB == 3 ? skip : 0) : nt;
+                    auto chain_of = [&](int e) { return C::NSB == 3 && skip && e == turns - 1 ? 1 : e & 1; };
+                    auto tile_of = [&](int e) { return two ? (C::NSB == 3 && skip && e == turns - 1 ? nt - 1 : e >> 1) : e; };
+                    for (int e = 0; e < turns + C::NSB; ++e) {
+                        const int ev = e - C::NSB;
+                        if (ev >= 0) {
+                            const int l = chain_of(ev), iv = tile_of(ev);
+                            if (!two || l == 1 || iv < nt0) {
+                                const uint32_t vseq = seq0 + 2u * (uint32_t)iv + 1u, vs = vseq % ns;
+                                if ((!two || l == 0 || iv >= nt0) && !(ok = mbar_wait(bar_full(vs), (vseq / ns) & 1, s_abort, p.status))) break;
+                                // the unit before is done with this chain's accumulator; a chain without a tile of this unit takes its turn
+                                // on the barrier here too
+                                if (ev < 2 && uq > 0 && !(ok = mbar_wait(bar_ofree(l), (uq - 1) & 1, s_abort, p.status))) break;
+                                if (turns < 2 && uq > 0 && !(ok = mbar_wait(bar_ofree(1), (uq - 1) & 1, s_abort, p.status))) break;
+                                const int k = C::NSB == 3 ? (int)((turn0 + (uint32_t)ev) % 3u) : l;
+                                const uint32_t parity = C::NSB == 3 ? ((turn0 + (uint32_t)ev) / 3u) & 1u : c_p[l]++ & 1u;
+                                const uint32_t vdesc = desc_lo(slot_base(vs), 1024), o_at = tmem + C::O_COL + l * D, p_at = tmem + k * 128;
+                                if (!(ok = mbar_wait(bar_pready(k), parity, s_abort, p.status))) break;
+                                tc_fence_after();
+                                mma_pv_halves_block<D>(o_at, p_at, vdesc, idesc_o, ev < 2 ? 0u : 1u);
+                                if (!two || l == 1) tc_commit(bar_free(vs));
+                                if (C::NSB == 3) tc_commit(bar_pvdone(k));
+                                if (iv >= (two && l == 0 ? nt0 : nt) - 1) tc_commit(two ? bar_odone(l) : bar_odone_both);
+                            }
                         }
-                        if (ik < mine) {
-                            const uint32_t kseq = seq0 + 2u * (uint32_t)ik, ks = kseq % ns;
-                            if (!two || l == 0 || ik >= nt0) {
-                                if (!(ok = mbar_wait(bar_full(ks), (kseq / ns) & 1, s_abort, p.status))) break;
-                                tc_fence_after();
+                        if (e < turns) {
+                            const int l = chain_of(e), ik = tile_of(e);
+                            if (!two || l == 1 || ik < nt0) {
+                                const uint32_t kseq = seq0 + 2u * (uint32_t)ik, ks = kseq % ns;
+                                if (!two || l == 0 || ik >= nt0) {
+                                    if (!(ok = mbar_wait(bar_full(ks), (kseq / ns) & 1, s_abort, p.status))) break;
+                                    tc_fence_after();
+                                }
+                                if (two && e == 1) {
+                                    if (!(ok = mbar_wait(bar_qfull(1), c_q1++ & 1, s_abort, p.status))) break;
+                                    tc_fence_after();
+                                }
+                                const int k = C::NSB == 3 ? (int)((turn0 + (uint32_t)e) % 3u) : l;
+                                mma_s_grouped_block<D>(tmem + k * 128, desc_lo(sbase + C::OFF_Q + (two ? l : 0) * C::Q_BYTES, 16), desc_lo(slot_base(ks), 16), idesc_s);
+                                tc_commit(bar_sfull(k));
+                                if (!two || l == 1) tc_commit(bar_free(ks));
+                                if (ik == (two && l == 0 ? nt0 : nt) - 1) tc_commit(bar_qfree(two ? l : 0));
                             }
-                            if (two && e == 1) {
-                                if (!(ok = mbar_wait(bar_qfull(1), c_q1++ & 1, s_abort, p.status))) break;
-                                tc_fence_after();
-                            }
-                            mma_s_grouped_block<D>(tmem + l * 128, desc_lo(sbase + C::OFF_Q + (two ? l : 0) * C::Q_BYTES, 16), desc_lo(slot_base(ks), 16), idesc_s);
-                            tc_commit(bar_sfull(l));
-                            if (!two || l == 1) tc_commit(bar_free(ks));
-                            if (ik == mine - 1) tc_commit(bar_qfree(two ? l : 0));
                         }
                     }
+                    turn0 += (uint32_t)turns;
                     if (!ok) break;
                     ++uq;
                 }
@@ -315,6 +336,7 @@ __global__ void __launch_bounds__(kThreads, 1) cb_chunk_tc_kernel(const CbChunkP
         constexpr int CW = D / 4;                             // accumulator columns handled at a time
         const bool out32 = (reinterpret_cast<uintptr_t>(p.out) & 31u) == 0;
         uint32_t c_s = 0, c_od = 0, c_ob = 0, uq = 0;         // completions consumed: S of this chain, o_done of this chain, o_done_both
+        uint32_t turn0 = 0;                                   // three S buffers: turns of both chains in the units before
         // The pair's barrier; k numbers the barriers between two tiles, so that what a warp notes before it waits only grows.
         auto pair_sync = [&](bool v, uint32_t k) {
             if (lane == 0) s_pair[sw] = (int)(4u * (c_s + uq) + k);
@@ -334,13 +356,24 @@ __global__ void __launch_bounds__(kThreads, 1) cb_chunk_tc_kernel(const CbChunkP
             const bool row_valid = row < RT && token < u->n;
             const bool warp_active = (wq * 32) < RT && first + token_of(wq * 32) < u->n;   // row 0 of the warp is valid
             const int limit = u->ctx + token + 1;             // keys that this row sees
-            const uint32_t ts = tmem + l * 128 + lane_addr, tsh = ts + 64 * hf;
             const uint32_t tm_O = tmem + C::O_COL + l * D + lane_addr;
             // the tile in whose last page there are slots behind the sequence's last token, for the warp that clears them
             const int unclean = u->dirty && hf == 0 && wq == 0 && (!two || l == u->skip) ? u->tiles - 1 : -1;
+            uint32_t turn = turn0 + l;                        // of the chain's next tile, every second one
+            const int last_out = two && l == 1 && u->skip ? t1 - 1 : -1;   // but for a last tile that the first chain leaves out
             float m_used = -INFINITY, lsum = 0.f;
             for (int i = tfirst; i < t1; i += step) {
-                if (!(ok = mbar_wait(bar_sfull(l), c_s & 1, s_abort, p.status))) break;
+                // this turn's S buffer, by the issuer's count of turns
+                int k = l;
+                uint32_t parity = c_s & 1;
+                if constexpr (C::NSB == 3) {
+                    const uint32_t at = turn - (i == last_out ? 1u : 0u);
+                    k = (int)(at % 3u);
+                    parity = (at / 3u) & 1u;
+                    turn += 2;
+                }
+                const uint32_t ts = tmem + k * 128 + lane_addr, tsh = ts + 64 * hf;
+                if (!(ok = mbar_wait(bar_sfull(k), parity, s_abort, p.status))) break;
                 ++c_s;
                 if (warp_active) {
                     tc_fence_after();
@@ -432,7 +465,13 @@ __global__ void __launch_bounds__(kThreads, 1) cb_chunk_tc_kernel(const CbChunkP
                         const float alpha = need ? ex2(m_used - mloc) : 1.0f;
                         if (need) m_used = mloc;
                         if (i > tfirst && __any_sync(CB_FULL, need)) {
-                            // O is complete up to the chain's previous tile; each of the two threads rescales half of the columns
+                            // O is complete up to the chain's previous tile, whose product went out before this S, or, with three buffers, behind it;
+                            // each of the two threads rescales half of the columns
+                            if constexpr (C::NSB == 3) {
+                                const uint32_t prev = turn - 4;   // of this chain; no turn before the last is out of step
+                                if (!(ok = mbar_wait(bar_pvdone((int)(prev % 3u)), (prev / 3u) & 1u, s_abort, p.status))) break;
+                                tc_fence_after();
+                            }
 #pragma unroll 1
                             for (int c = 0; c < 2; ++c) {
                                 uint32_t o[CW];
@@ -465,7 +504,7 @@ __global__ void __launch_bounds__(kThreads, 1) cb_chunk_tc_kernel(const CbChunkP
                 }
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(bar_pready(l));
+                if (lane == 0) mbar_arrive(bar_pready(k));
             }
             if (!ok) break;
             // ---- epilogue of this unit's share
@@ -720,6 +759,7 @@ __global__ void __launch_bounds__(kThreads, 1) cb_chunk_tc_kernel(const CbChunkP
                 }
                 break;
             }
+            if constexpr (C::NSB == 3) turn0 += (uint32_t)(two ? 2 * (u->t1 - t0) - u->skip : u->t1 - t0);
             tc_fence_before();
             __syncwarp();
             if (lane == 0) {                                  // 16 arrivals per unit either way

@@ -39,6 +39,7 @@ struct CbChunkParams {
     int one;                  // every chunk fits one row tile, by max_chunk
     int nc;                   // persistent CTAs
     int cs;                   // > 0: few units, so many CTAs share each (cb_chunk_share); 0: equal ranges of the positions
+    uint32_t cs_inv, hkv_inv; // x / cs = __umulhi(x, cs_inv) for x < 2^16, and for Hkv
     int w1, w2, d1, d2;       // positions per key tile of a unit with one or two row tiles, and which of them decides whose tile it is
     float* part;              // partial outputs of units shared between CTAs; tickets and turn as in tree attention, whose scratch this is
     uint32_t *part_ticket, *part_turn;

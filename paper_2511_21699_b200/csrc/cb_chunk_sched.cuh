@@ -197,15 +197,15 @@ __device__ __forceinline__ void cb_chunk_range(const CbChunkParams& p, int cta, 
 // Launches of few units of one row tile (single tokens of a small batch) are not cut into ranges: unit u = (sequence, kv head) has CTAs
 // u cs .. u cs + cs - 1, which take equal parts of its tiles.  A CTA then needs one sequence's lengths and next to no arithmetic before its
 // first copy, and no CTA has more than one unit to see to.
-__device__ __forceinline__ bool cb_chunk_share(const CbChunkParams& p, int cta, CbChunkUnit* u, CbChunkShape* s, int* ctas) {
-    const int unit = cta / p.cs, rank = cta - unit * p.cs;
-    u->b = unit / p.Hkv; u->kh = unit - u->b * p.Hkv; u->rg = 0;
-    *s = cb_chunk_shape(p, u->b);
+__device__ __forceinline__ bool cb_chunk_share(const CbChunkParams& p, int b, int kh, int rank, CbChunkUnit* u, CbChunkShape* s, int* ctas) {
+    u->b = b; u->kh = kh; u->rg = 0;
+    *s = cb_chunk_shape(p, b);
     if (s->RG == 0) return false;
-    const int tiles = s->tiles(0);
-    *ctas = min(p.cs, tiles);
-    if (rank >= *ctas) return false;
-    u->t0 = (int)((long long)tiles * rank / *ctas); u->t1 = (int)((long long)tiles * (rank + 1) / *ctas);
+    const int tiles = s->tiles(0), n = min(p.cs, tiles);
+    *ctas = n;
+    if (rank >= n) return false;
+    // (tiles below 2^23 and ranks below 32: the products fit 32 bits)
+    u->t0 = (int)cb_quot((long long)(tiles * rank), n); u->t1 = (int)cb_quot((long long)(tiles * (rank + 1)), n);
     return true;
 }
 // How many CTAs share a unit: what the longest unit's share of tiles takes, bandwidth shared by all, and what putting the parts together

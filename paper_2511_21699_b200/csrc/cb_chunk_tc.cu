@@ -275,11 +275,11 @@ __global__ void __launch_bounds__(kThreads, 1) cb_chunk_tc_kernel(const CbChunkP
             if (p.cs > 0) {
                 CbChunkShape s;
                 int np = 0;
-                const bool has = cb_chunk_share(p, cta, &x, &s, &np);
+                const int unit = p.cs == 1 ? cta : (int)__umulhi((uint32_t)cta, p.cs_inv), b = p.Hkv == 1 ? unit : (int)__umulhi((uint32_t)unit, p.hkv_inv), cf = unit * p.cs;
+                const bool has = cb_chunk_share(p, b, unit - b * p.Hkv, cta - cf, &x, &s, &np);
                 error = s.error;
                 if (lane == 0 && has) {
                     volatile ChunkUnit* u = &s_units[0];
-                    const int cf = cta / p.cs * p.cs;
                     u->cf = cf; u->np = np; u->xpos = -1; u->ticket = ticket_set + cf * 16;
                     publish(x, s);
                     load_queries(x, s);
@@ -336,7 +336,7 @@ __global__ void __launch_bounds__(kThreads, 1) cb_chunk_tc_kernel(const CbChunkP
         constexpr int CW = D / 4;                             // accumulator columns handled at a time
         const bool out32 = (reinterpret_cast<uintptr_t>(p.out) & 31u) == 0;
         uint32_t c_s = 0, c_od = 0, c_ob = 0, uq = 0;         // completions consumed: S of this chain, o_done of this chain, o_done_both
-        uint32_t turn0 = 0;                                   // three S buffers: turns of both chains in the units before
+        int turn0 = 0;                                        // three S buffers: turns of both chains in the units before, modulo 6
         // The pair's barrier; k numbers the barriers between two tiles, so that what a warp notes before it waits only grows.
         auto pair_sync = [&](bool v, uint32_t k) {
             if (lane == 0) s_pair[sw] = (int)(4u * (c_s + uq) + k);
@@ -359,7 +359,8 @@ __global__ void __launch_bounds__(kThreads, 1) cb_chunk_tc_kernel(const CbChunkP
             const uint32_t tm_O = tmem + C::O_COL + l * D + lane_addr;
             // the tile in whose last page there are slots behind the sequence's last token, for the warp that clears them
             const int unclean = u->dirty && hf == 0 && wq == 0 && (!two || l == u->skip) ? u->tiles - 1 : -1;
-            uint32_t turn = turn0 + l;                        // of the chain's next tile, every second one
+            int sb = turn0 + l;                               // the chain's next turn, every second one, modulo 6: buffer and phase
+            if (sb >= 6) sb -= 6;
             const int last_out = two && l == 1 && u->skip ? t1 - 1 : -1;   // but for a last tile that the first chain leaves out
             float m_used = -INFINITY, lsum = 0.f;
             for (int i = tfirst; i < t1; i += step) {
@@ -367,10 +368,10 @@ __global__ void __launch_bounds__(kThreads, 1) cb_chunk_tc_kernel(const CbChunkP
                 int k = l;
                 uint32_t parity = c_s & 1;
                 if constexpr (C::NSB == 3) {
-                    const uint32_t at = turn - (i == last_out ? 1u : 0u);
-                    k = (int)(at % 3u);
-                    parity = (at / 3u) & 1u;
-                    turn += 2;
+                    if (i == last_out) sb = sb == 0 ? 5 : sb - 1;
+                    k = sb >= 3 ? sb - 3 : sb;
+                    parity = sb >= 3;
+                    sb = sb >= 4 ? sb - 4 : sb + 2;           // the chain's next turn
                 }
                 const uint32_t ts = tmem + k * 128 + lane_addr, tsh = ts + 64 * hf;
                 if (!(ok = mbar_wait(bar_sfull(k), parity, s_abort, p.status))) break;
@@ -468,8 +469,8 @@ __global__ void __launch_bounds__(kThreads, 1) cb_chunk_tc_kernel(const CbChunkP
                             // O is complete up to the chain's previous tile, whose product went out before this S, or, with three buffers, behind it;
                             // each of the two threads rescales half of the columns
                             if constexpr (C::NSB == 3) {
-                                const uint32_t prev = turn - 4;   // of this chain; no turn before the last is out of step
-                                if (!(ok = mbar_wait(bar_pvdone((int)(prev % 3u)), (prev / 3u) & 1u, s_abort, p.status))) break;
+                                const int prev = (sb + (i == last_out ? 3 : 2)) % 6;   // the chain's turn before, four before the next one in sb (three, out of step)
+                                if (!(ok = mbar_wait(bar_pvdone(prev % 3), (uint32_t)(prev / 3), s_abort, p.status))) break;
                                 tc_fence_after();
                             }
 #pragma unroll 1
@@ -759,7 +760,7 @@ __global__ void __launch_bounds__(kThreads, 1) cb_chunk_tc_kernel(const CbChunkP
                 }
                 break;
             }
-            if constexpr (C::NSB == 3) turn0 += (uint32_t)(two ? 2 * (u->t1 - t0) - u->skip : u->t1 - t0);
+            if constexpr (C::NSB == 3) turn0 = (turn0 + (two ? 2 * (u->t1 - t0) - u->skip : u->t1 - t0)) % 6;
             tc_fence_before();
             __syncwarp();
             if (lane == 0) {                                  // 16 arrivals per unit either way
@@ -870,6 +871,8 @@ cb_status cb_chunk_launch_tensor(cb_ctx* ctx, const CbChunkParams& given, cudaSt
     cb_attn_weights(w);
     p.w1 = w.w1; p.w2 = w.w2; p.d1 = w.d1; p.d2 = w.d2;
     p.cs = p.one ? cb_chunk_pick_share((long long)p.B * p.Hkv, ((long long)p.max_keys + CB_KT - 1) / CB_KT, p.nc) : 0;
+    p.cs_inv = p.cs > 1 ? 0xFFFFFFFFu / (uint32_t)p.cs + 1u : 0u;      // exact for numerators below 2^16 (__umulhi); a divisor of 1 is set aside
+    p.hkv_inv = p.Hkv > 1 ? 0xFFFFFFFFu / (uint32_t)p.Hkv + 1u : 0u;
     p.part = ctx->d_attn_part; p.part_ticket = ctx->d_attn_ticket; p.part_turn = ctx->d_attn_turn;
     ChunkMaps maps;
     if (!encode_pool(&maps.k, p.k_pool, p) || !encode_pool(&maps.v, p.v_pool, p) || !encode_queries(&maps.q, p)) return CB_ERR_CUDA;

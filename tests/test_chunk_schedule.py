@@ -47,7 +47,7 @@ int main() {
                 CbChunkUnit u;
                 CbChunkShape s;
                 int np = 0;
-                if (cb_chunk_share(p, k, &u, &s, &np)) printf("%d %d %d %d %d %d %d ", k, u.b, u.kh, u.t0, u.t1, s.tiles(0), np);
+                if (cb_chunk_share(p, k / p.cs / p.Hkv, k / p.cs % p.Hkv, k % p.cs, &u, &s, &np)) printf("%d %d %d %d %d %d %d ", k, u.b, u.kh, u.t0, u.t1, s.tiles(0), np);
             }
         } else if (what == 1) {
             long long n;

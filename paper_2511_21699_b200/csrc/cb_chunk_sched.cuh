@@ -125,6 +125,23 @@ struct CbChunkWalker {
         }
         return false;
     }
+    // The same with two whole units of one row tile at a time, of neighbouring heads, where the range holds the second one's tiles as well: a chain
+    // each, so that what lies between two units (some 7 k cycles of a unit of one tile) is paid once for both.
+    __device__ __forceinline__ bool next_pair(const CbChunkParams& p, CbChunkUnit* u, bool* heads) {
+        *heads = false;
+        if (!next(p, u)) return false;
+        const int tiles = s.tiles(u->rg);
+        if (s.two_rows(u->rg) || u->t0 > 0 || u->t1 < tiles || u->kh + 1 >= p.Hkv || g >= g1) return true;
+        const int vt = s.unit(u->rg);                         // (pos is at the next head's unit now)
+        if (pos + s.dec(u->rg) + (long long)(tiles - 1) * s.wt(u->rg) >= g1) return true;
+        g = min(pos + vt, g1);
+        if (g < g1) {
+            pos += vt;
+            if (++kh == p.Hkv) { kh = 0; ++rg; }
+        }
+        *heads = true;
+        return true;
+    }
 };
 
 // This CTA's range and the walker at its start, by a whole warp (every lane gets both), and the cuts.  *error: what this lane found wrong with a

@@ -3,7 +3,7 @@
 // Persistent kernel, one CTA per SM, built like tree attention (cb_attn_tc.cu, which explains the chains and their costs): a CTA holds up
 // to two 128-row query tiles of a unit (128 / G tokens times the G query heads of a kv head) and streams the unit's 128-key tiles through a
 // ring of shared-memory slots; two chains S = Q K^T -> softmax -> O += P V run side by side, each with a row tile of its own, or, in a unit
-// with one row tile (single tokens, the end of a chunk), with every second key tile.  The split over the CTAs is in cb_chunk_sched.cuh; the
+// with one row tile (single tokens, the end of a chunk), with every second key tile, or with the unit of a head of its own.  The split over the CTAs is in cb_chunk_sched.cuh; the
 // CTAs of a shared unit put their unnormalised parts together through memory, the last one to come writes the rows.
 //
 // Warp roles (640 threads): warp 0 copies K tiles, warp 3 V tiles, warp 1 issues the products, warp 2 walks the units, publishes them to all
@@ -23,7 +23,9 @@
 
 namespace {
 
-// A unit as its roles see it (nrt = 0: no more units).
+constexpr int kTwoHeads = 3;                                  // the whole units of heads kh and kh + 1, of one row tile, a chain each
+
+// A unit as its roles see it (nrt: row tiles, or kTwoHeads; 0: no more units).
 struct ChunkUnit {
     int b, kh, rg, t0, t1, tiles, nrt;
     int row0, n, ctx, end;    // first packed row, new and cached tokens of the sequence, keys that the unit sees
@@ -141,7 +143,7 @@ __global__ void __launch_bounds__(kThreads, 1) cb_chunk_tc_kernel(const CbChunkP
             for (uint32_t uq = 0; (ok = mbar_wait(bar_ufull(uq % kUnitRing), (uq / kUnitRing) & 1, s_abort, p.status)); ++uq) {
                 const volatile ChunkUnit* u = &s_units[uq % kUnitRing];
                 if (u->nrt == 0) break;
-                const int t0 = u->t0, t1 = u->t1, kh = u->kh, npages = (u->end + 15) / 16;
+                const int t0 = u->t0, t1 = u->t1, kh = u->kh, npages = (u->end + 15) / 16, heads = u->nrt == kTwoHeads ? 2 : 1;   // their tiles come in turn
                 const int32_t* bt = p.block_table + (size_t)u->b * p.max_pages;
                 uint32_t seq = (uint32_t)u->seq0 + (isV ? 1u : 0u);
                 // the page number is fetched one tile ahead of the copy that depends on it; out of the pool, the copy fills zeros
@@ -151,14 +153,16 @@ __global__ void __launch_bounds__(kThreads, 1) cb_chunk_tc_kernel(const CbChunkP
                     return (uint32_t)page < (uint32_t)p.num_pages ? page : p.num_pages;
                 };
                 int page_next = page_of(t0);
-                for (int i = t0; i < t1; ++i, seq += 2) {
+                for (int i = t0; i < t1 && ok; ++i) {
                     const int page = page_next;
                     if (i + 1 < t1) page_next = page_of(i + 1);
-                    const uint32_t sl = seq % ns;
-                    if (seq >= ns && !(ok = mbar_wait(bar_free(sl), (seq / ns - 1) & 1, s_abort, p.status))) break;
-                    if (lane == 0) mbar_expect_tx(bar_full(sl), C::TILE_BYTES);
-                    __syncwarp();
-                    if (active) tma_load_5d(slot_base(sl) + lane * 2 * GROUP, isV ? &maps.v : &maps.k, bar_full(sl), 0, 0, 0, page * 2, kh);
+                    for (int hd = 0; hd < heads; ++hd, seq += 2) {
+                        const uint32_t sl = seq % ns;
+                        if (seq >= ns && !(ok = mbar_wait(bar_free(sl), (seq / ns - 1) & 1, s_abort, p.status))) break;
+                        if (lane == 0) mbar_expect_tx(bar_full(sl), C::TILE_BYTES);
+                        __syncwarp();
+                        if (active) tma_load_5d(slot_base(sl) + lane * 2 * GROUP, isV ? &maps.v : &maps.k, bar_full(sl), 0, 0, 0, page * 2, kh + hd);
+                    }
                 }
                 if (!ok) break;
             }
@@ -172,12 +176,12 @@ __global__ void __launch_bounds__(kThreads, 1) cb_chunk_tc_kernel(const CbChunkP
                     const volatile ChunkUnit* u = &s_units[uq % kUnitRing];
                     const int nrt = u->nrt;
                     if (nrt == 0) break;
-                    const bool two = nrt == 2;
-                    const int nt = u->t1 - u->t0;
+                    const bool two = nrt == 2, heads = nrt == kTwoHeads;
+                    const int nt = heads ? 2 * u->tiles : u->t1 - u->t0;          // key tiles that come through the ring
                     const uint32_t seq0 = (uint32_t)u->seq0;
                     const int nt0 = nt - u->skip;             // tiles of the first chain
                     if (!(ok = mbar_wait(bar_qfull(0), uq & 1, s_abort, p.status))) break;
-                    // Turn e is tile e / 2 for chain e & 1 with two row tiles, else tile e for chain e & 1.  Its S goes out behind the P V of NSB turns before,
+                    // Turn e is tile e / 2 for chain e & 1 with two row tiles, else the e-th tile for chain e & 1.  Its S goes out behind the P V of NSB turns before,
                     // whose buffer it takes.  A tile that the first chain leaves out is a turn of nobody's; with three buffers, which
                     // go by the count of turns, it is none, and the last turn is the second chain's whatever its number.
                     const int skip = nt - nt0, turns = two ? 2 * nt - (C::NSB == 3 ? skip : 0) : nt;
@@ -202,7 +206,7 @@ __global__ void __launch_bounds__(kThreads, 1) cb_chunk_tc_kernel(const CbChunkP
                                 mma_pv_halves_block<D>(o_at, p_at, vdesc, idesc_o, ev < 2 ? 0u : 1u);
                                 if (!two || l == 1) tc_commit(bar_free(vs));
                                 if (C::NSB == 3) tc_commit(bar_pvdone(k));
-                                if (iv >= (two && l == 0 ? nt0 : nt) - 1) tc_commit(two ? bar_odone(l) : bar_odone_both);
+                                if (iv >= (two && l == 0 ? nt0 : nt) - (heads ? 2 : 1)) tc_commit(two || heads ? bar_odone(l) : bar_odone_both);
                             }
                         }
                         if (e < turns) {
@@ -213,15 +217,15 @@ __global__ void __launch_bounds__(kThreads, 1) cb_chunk_tc_kernel(const CbChunkP
                                     if (!(ok = mbar_wait(bar_full(ks), (kseq / ns) & 1, s_abort, p.status))) break;
                                     tc_fence_after();
                                 }
-                                if (two && e == 1) {
+                                if (nrt > 1 && e == 1) {
                                     if (!(ok = mbar_wait(bar_qfull(1), c_q1++ & 1, s_abort, p.status))) break;
                                     tc_fence_after();
                                 }
                                 const int k = C::NSB == 3 ? (int)((turn0 + (uint32_t)e) % 3u) : l;
-                                mma_s_grouped_block<D>(tmem + k * 128, desc_lo(sbase + C::OFF_Q + (two ? l : 0) * C::Q_BYTES, 16), desc_lo(slot_base(ks), 16), idesc_s);
+                                mma_s_grouped_block<D>(tmem + k * 128, desc_lo(sbase + C::OFF_Q + (nrt > 1 ? l : 0) * C::Q_BYTES, 16), desc_lo(slot_base(ks), 16), idesc_s);
                                 tc_commit(bar_sfull(k));
                                 if (!two || l == 1) tc_commit(bar_free(ks));
-                                if (ik == (two && l == 0 ? nt0 : nt) - 1) tc_commit(bar_qfree(two ? l : 0));
+                                if (ik >= (two && l == 0 ? nt0 : nt) - (heads ? 2 : 1)) tc_commit(bar_qfree(nrt > 1 ? l : 0));
                             }
                         }
                     }
@@ -239,34 +243,34 @@ __global__ void __launch_bounds__(kThreads, 1) cb_chunk_tc_kernel(const CbChunkP
             int error = 0, seq = 0;
             uint32_t uq = 0;
             // What all roles need of a unit; a shared one's holder of the first tile and number of CTAs are set before.
-            auto publish = [&](const CbChunkUnit& x, const CbChunkShape& s) {
+            auto publish = [&](const CbChunkUnit& x, const CbChunkShape& s, bool heads) {
                 volatile ChunkUnit* u = &s_units[uq % kUnitRing];
-                const int tiles = s.tiles(x.rg), nrt = s.two_rows(x.rg) ? 2 : 1;
+                const int tiles = s.tiles(x.rg), nrt = s.two_rows(x.rg) ? 2 : (heads ? kTwoHeads : 1);
                 u->b = x.b; u->kh = x.kh; u->rg = x.rg; u->t0 = x.t0; u->t1 = x.t1; u->tiles = tiles; u->nrt = nrt;
                 u->row0 = s.row0; u->n = s.n; u->ctx = s.ctx; u->end = s.end(x.rg);
                 u->seq0 = seq;
                 u->skip = nrt == 2 && x.t1 == tiles && x.t1 - x.t0 > 1 && (tiles - 1) * CB_KT >= s.ctx + (2 * x.rg + 1) * p.NPT;
                 u->dirty = max((s.end(x.rg) + 15) / 16 * 16 - (s.ctx + s.n), 0);
-                seq += 2 * (x.t1 - x.t0);
+                seq += (heads ? 4 : 2) * (x.t1 - x.t0);
                 mbar_arrive(bar_ufull(uq % kUnitRing));
             };
             // A unit's query tiles, each when the one before it there has been read; the next unit's are asked into L2 as soon as it is known.
             uint32_t n_q1 = 0;
-            auto query_box = [&](const CbChunkUnit& x, const CbChunkShape& s, int k, int db, bool ahead) {
-                const int c0 = db * 64, c1 = x.kh * p.G, c2 = s.row0 + (2 * x.rg + k) * p.NPT;
+            auto query_box = [&](const CbChunkUnit& x, const CbChunkShape& s, bool heads, int k, int db, bool ahead) {
+                const int c0 = db * 64, c1 = (x.kh + (heads ? k : 0)) * p.G, c2 = s.row0 + (2 * x.rg + (heads ? 0 : k)) * p.NPT;
                 if (ahead) asm volatile("cp.async.bulk.prefetch.tensor.4d.L2.global.tile [%0, {%1, %2, %3, %4}];" ::"l"(&maps.q), "r"(c0), "r"(c1), "r"(c2), "r"(0) : "memory");
                 else tma_load_4d(sbase + C::OFF_Q + k * C::Q_BYTES + db * (CB_MT * 128), &maps.q, bar_qfull(k), c0, c1, c2, 0);
             };
-            auto load_queries = [&](const CbChunkUnit& x, const CbChunkShape& s) {
-                const int nrt = s.two_rows(x.rg) ? 2 : 1;
+            auto load_queries = [&](const CbChunkUnit& x, const CbChunkShape& s, bool heads) {
+                const int nrt = s.two_rows(x.rg) || heads ? 2 : 1;
                 if (uq > 0)
                     for (int k = 0; k < nrt; ++k)
-                        for (int db = 0; db < C::DB; ++db) query_box(x, s, k, db, true);
+                        for (int db = 0; db < C::DB; ++db) query_box(x, s, heads, k, db, true);
                 for (int k = 0; k < nrt; ++k) {
                     const uint32_t before = k == 0 ? uq : n_q1;
                     if (before > 0 && !(ok = mbar_wait(bar_qfree(k), (before - 1) & 1, s_abort, p.status))) return;
                     mbar_expect_tx(bar_qfull(k), (uint32_t)(C::DB * RT * 128));
-                    for (int db = 0; db < C::DB; ++db) query_box(x, s, k, db, false);
+                    for (int db = 0; db < C::DB; ++db) query_box(x, s, heads, k, db, false);
                     if (k == 1) ++n_q1;
                 }
             };
@@ -280,8 +284,8 @@ __global__ void __launch_bounds__(kThreads, 1) cb_chunk_tc_kernel(const CbChunkP
                 if (lane == 0 && has) {
                     volatile ChunkUnit* u = &s_units[0];
                     u->cf = cf; u->np = np; u->xpos = -1; u->ticket = ticket_set + cf * 16;
-                    publish(x, s);
-                    load_queries(x, s);
+                    publish(x, s, false);
+                    load_queries(x, s, false);
                     ++uq;
                 }
             } else {
@@ -291,7 +295,8 @@ __global__ void __launch_bounds__(kThreads, 1) cb_chunk_tc_kernel(const CbChunkP
                 if (cta > 0) error = 0;
                 if (lane == 0) {
                     *s_tot = cuts.total;
-                    while (ok && wk.next(p, &x)) {
+                    bool heads = false;
+                    while (ok && wk.next_pair(p, &x, &heads)) {
                         const CbChunkShape& s = wk.s;         // of the unit's sequence: the walker goes on when it is asked again
                         const int tiles = s.tiles(x.rg), wt = s.wt(x.rg);
                         if (!(x.t0 == 0 && x.t1 == tiles)) {
@@ -306,8 +311,8 @@ __global__ void __launch_bounds__(kThreads, 1) cb_chunk_tc_kernel(const CbChunkP
                             u->wt = wt;
                             u->ticket = ticket_set + cf * 16;
                         }
-                        publish(x, s);
-                        load_queries(x, s);
+                        publish(x, s, heads);
+                        load_queries(x, s, heads);
                         if (!ok) break;
                         ++uq;
                     }
@@ -346,8 +351,8 @@ __global__ void __launch_bounds__(kThreads, 1) cb_chunk_tc_kernel(const CbChunkP
             if (!(ok = mbar_wait(bar_ufull(uq % kUnitRing), (uq / kUnitRing) & 1, s_abort, p.status))) break;
             const volatile ChunkUnit* u = &s_units[uq % kUnitRing];   // read again where it is needed: registers are short
             if (u->nrt == 0) break;
-            const bool two = u->nrt == 2;
-            const int first = (2 * u->rg + (two ? l : 0)) * p.NPT;    // this chain's row tile: its first token
+            const bool two = u->nrt > 1;                      // a chain has rows of its own: a row tile, or a head's only one
+            const int first = (2 * u->rg + (u->nrt == 2 ? l : 0)) * p.NPT;   // its first token
             const int step = two ? 1 : 2, tfirst = u->t0 + (two ? 0 : l);
             const int t1 = u->t1 - (l == 0 ? u->skip : 0);
             const int nfull = (u->ctx + first + 1) / CB_KT;   // tiles that all its rows see whole
@@ -357,7 +362,7 @@ __global__ void __launch_bounds__(kThreads, 1) cb_chunk_tc_kernel(const CbChunkP
             const int limit = u->ctx + token + 1;             // keys that this row sees
             const uint32_t tm_O = tmem + C::O_COL + l * D + lane_addr;
             // the tile in whose last page there are slots behind the sequence's last token, for the warp that clears them
-            const int unclean = u->dirty && hf == 0 && wq == 0 && (!two || l == u->skip) ? u->tiles - 1 : -1;
+            const int unclean = u->dirty && hf == 0 && wq == 0 && (u->nrt != 2 || l == u->skip) ? u->tiles - 1 : -1;
             int sb = turn0 + l;                               // the chain's next turn, every second one, modulo 6: buffer and phase
             if (sb >= 6) sb -= 6;
             const int last_out = two && l == 1 && u->skip ? t1 - 1 : -1;   // but for a last tile that the first chain leaves out
@@ -490,7 +495,7 @@ __global__ void __launch_bounds__(kThreads, 1) cb_chunk_tc_kernel(const CbChunkP
                 }
                 if (i == unclean) {
                     // Zeros there before any product reads the tile; with two row tiles by the chain whose product comes first.
-                    const uint32_t vseq = (uint32_t)u->seq0 + 2u * (uint32_t)(i - u->t0) + 1u, vs = vseq % ns;
+                    const uint32_t vseq = (uint32_t)u->seq0 + 2u * (uint32_t)(u->nrt == kTwoHeads ? 2 * i + l : i - u->t0) + 1u, vs = vseq % ns;
                     if (!(ok = mbar_wait(bar_full(vs), (vseq / ns) & 1, s_abort, p.status))) break;
                     const int r0 = u->ctx + u->n - i * CB_KT, pieces = u->dirty * (D / 8);
                     for (int k = lane; k < pieces; k += 32) {
@@ -506,7 +511,7 @@ __global__ void __launch_bounds__(kThreads, 1) cb_chunk_tc_kernel(const CbChunkP
             }
             if (!ok) break;
             // ---- epilogue of this unit's share
-            const int t0 = u->t0, h = u->kh * p.G + row - token_of(row) * p.G;
+            const int t0 = u->t0, h = (u->kh + (u->nrt == kTwoHeads ? l : 0)) * p.G + row - token_of(row) * p.G;
             const bool whole = t0 == 0 && u->t1 == u->tiles;
             const size_t at_row = (size_t)(u->row0 + (row_valid ? token : 0)) * p.Hq + h;
             // this thread's columns of the output row, 16 at a time: half a row with two row tiles, a quarter with one

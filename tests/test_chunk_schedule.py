@@ -56,6 +56,7 @@ int main() {
             printf("%lld ", cb_floor_sum(n, a, b));
         } else {
             CbChunkParams p = {};
+            const bool pairs = what == 4;
             if (scanf("%d %d %d %d %d %d %d %d", &p.B, &p.G, &p.Hkv, &p.D, &p.nc, &p.max_chunk, &p.max_keys, &p.n_rows) != 8) return 1;
             std::vector<int> q(p.B + 1), c(p.B);
             for (int& x : q) if (scanf("%d", &x) != 1) return 1;
@@ -79,11 +80,12 @@ int main() {
                     if (lane == 7) { wk = x; cuts = t; }
                 });
                 CbChunkUnit u;
-                while (wk.next(p, &u)) {
+                bool heads = false;
+                while (pairs ? wk.next_pair(p, &u, &heads) : wk.next(p, &u)) {
                     const CbChunkShape& s = wk.s;
                     const int tiles = s.tiles(u.rg), wt = s.wt(u.rg), cf = cuts.of(u.first);
                     const int np = cuts.total >= (long long)p.nc * wt ? cuts.of(u.first + (long long)(tiles - 1) * wt) - cf + 1 : tiles;
-                    printf("%d %d %d %d %d %d %d %d %d %d %d %d ", k, u.b, u.kh, u.rg, u.t0, u.t1, tiles, s.two_rows(u.rg) ? 2 : 1, s.row0, s.end(u.rg), cf, np);
+                    printf("%d %d %d %d %d %d %d %d %d %d %d %d ", k, u.b, u.kh, u.rg, u.t0, u.t1, tiles, heads ? 3 : (s.two_rows(u.rg) ? 2 : 1), s.row0, s.end(u.rg), cf, np);
                 }
             }
             printf("\n%d", error);
@@ -171,7 +173,19 @@ def test_who_works_on_what(shim, G, hkv, D, new, ctx):
             units, error = shim(text).split("\n")[:2]
             got = sorted(tuple(int(y) for y in x) for x in np.array(units.split(), np.int64).reshape(-1, 12))
             assert int(error) == 0
-            assert got == _plain(G, hkv, D, nc, max_chunk, q, ctx)
+            want = _plain(G, hkv, D, nc, max_chunk, q, ctx)
+            assert got == want
+            # whole units of one row tile taken two heads at a time, from the front, wherever the next head's is whole here too
+            flat = sorted(want, key=lambda x: (x[0], x[1], x[3], x[2]))
+            paired, k = [], 0
+            while k < len(flat):
+                x = flat[k]
+                y = flat[k + 1] if k + 1 < len(flat) else None
+                both = (y is not None and x[7] == 1 and (x[4], x[5]) == (0, x[6]) and (y[0], y[1], y[2], y[3], y[4], y[5]) == (x[0], x[1], x[2] + 1, x[3], 0, x[6]))
+                paired.append(x[:7] + (3,) + x[8:] if both else x)
+                k += 1 + both
+            units, _ = shim(text.replace("2 ", "4 ", 1)).split("\n")[:2]
+            assert [tuple(int(y) for y in x) for x in np.array(units.split(), np.int64).reshape(-1, 12)] == paired
             have = sorted((x[1], x[2], x[3], t) for x in got for t in range(x[4], x[5]))    # every tile once
             assert len(have) == len(set(have)) == sum(x[6] for x in {(y[1], y[2], y[3]): y for y in got}.values())
 

@@ -80,10 +80,11 @@ extern "C" cb_status cb_create(const cb_config* cfg, void* dev_workspace, size_t
     c->ws = (char*)dev_workspace;
     c->ws_bytes = bytes;
     if (cudaGetDevice(&c->device) != cudaSuccess) { delete c; return CB_ERR_CUDA; }
-    cudaDeviceProp prop;
-    if (cudaGetDeviceProperties(&prop, c->device) != cudaSuccess) { delete c; return CB_ERR_CUDA; }
-    if (prop.major != 10) { delete c; return CB_ERR_UNSUPPORTED; }
-    c->num_sms = prop.multiProcessorCount;
+    // (two attributes, not cudaGetDeviceProperties, which reads them all)
+    int major = 0;
+    if (cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, c->device) != cudaSuccess ||
+        cudaDeviceGetAttribute(&c->num_sms, cudaDevAttrMultiProcessorCount, c->device) != cudaSuccess) { delete c; return CB_ERR_CUDA; }
+    if (major != 10) { delete c; return CB_ERR_UNSUPPORTED; }
     CbTables& t = c->tables;
     t.hdr = (uint32_t*)(c->ws + L.off_hdr);
     t.index = (uint32_t*)(c->ws + L.off_index);

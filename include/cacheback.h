@@ -370,8 +370,9 @@ typedef struct {
  *   q_out       bf16 [n_rows, Hq, D]            may be q itself where q_stride = Hq * D
  *   k_pool, v_pool  bf16 [num_pages, P, Hkv, D] written at the new positions only
  * Rows that belong to no sequence (before q_start[0], from q_start[batch] on) are left as they were.  A sequence whose pages cannot
- * hold the new tokens is left alone (no row of it is written) and CB_ERR_KV_FULL is recorded in the device status; a row whose position
- * the rope table does not have, or whose page lies outside the pool, is left alone and CB_ERR_INVALID_ARG recorded.
+ * hold the new tokens is left alone (no row of it is written) and CB_ERR_KV_FULL is recorded in the device status; one whose range is not
+ * inside [0, n_rows] or whose ctx_len is negative, and a row whose position the rope table does not have or whose page lies outside the
+ * pool, are left alone and CB_ERR_INVALID_ARG recorded.
  */
 typedef struct {
     cb_qkv_rows rows;

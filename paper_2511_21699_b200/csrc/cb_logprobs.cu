@@ -401,6 +401,7 @@ __global__ void __launch_bounds__(kThreads, 4) cb_logprobs_kernel(const LogprobP
     }
     if (p.cs > 1) {
         // The first CTA reads what the others have; they stay until it has.
+        __syncwarp();
         asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
         asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
         if (part == 0) {
@@ -425,6 +426,7 @@ __global__ void __launch_bounds__(kThreads, 4) cb_logprobs_kernel(const LogprobP
                 if (k != 0 && rank < p.K) s_top[rank] = k;
             }
         }
+        __syncwarp();
         asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
         if (part > 0) {
             asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
@@ -444,6 +446,7 @@ __global__ void __launch_bounds__(kThreads, 4) cb_logprobs_kernel(const LogprobP
             p.top_logprobs[(size_t)i * p.K + tid] = k == 0 ? -INFINITY : (value_of(k) - a.m) - log_s;
         }
     }
+    __syncwarp();
     if (p.cs > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 

@@ -87,13 +87,13 @@ __global__ void __launch_bounds__(32 * kRopeWarps) cb_rope_kernel(const RopePara
         const int b = cb_find_sequence(p.q_start, p.B, row, lane, p.ctx_len, &q0, &q1, &ctx);
         if (b < 0) return;
         if (row < q0 || row >= q1) return;                    // behind the last sequence
-        const bool full = (long long)ctx + q1 - q0 > (long long)p.max_pages * p.P;
+        const bool bad = ctx < 0 || q0 < 0 || q1 > p.n_rows, full = (long long)ctx + q1 - q0 > (long long)p.max_pages * p.P;
         pos = (long long)ctx + row - q0;
-        if (ctx < 0 || full || (p.rope && pos >= p.rope_len)) {
-            if (lane == 0) atomicCAS(p.status, 0u, (uint32_t)(ctx >= 0 && full ? CB_ERR_KV_FULL : CB_ERR_INVALID_ARG));
+        if (bad || full || (p.rope && pos >= p.rope_len)) {
+            if (lane == 0) atomicCAS(p.status, 0u, (uint32_t)(!bad && full ? CB_ERR_KV_FULL : CB_ERR_INVALID_ARG));
             return;
         }
-        const uint32_t at = (uint32_t)pos / (uint32_t)p.P;    // (a position is below 2^31: it fits the pages, or the sum would be full)
+        const uint32_t at = (uint32_t)pos / (uint32_t)p.P;    // (a position, the sum of two lengths, is below 2^32)
         const int page = p.block_table[(size_t)b * p.max_pages + at];
         if (page < 0 || page >= p.num_pages) {
             if (lane == 0) atomicCAS(p.status, 0u, (uint32_t)CB_ERR_INVALID_ARG);

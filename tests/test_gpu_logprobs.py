@@ -125,6 +125,16 @@ def test_forbidden_tokens_and_rows_without_a_value(dtype):
     assert bool(((got["top_ids"] >= -1) & (got["top_ids"] < V)).all()) and cb.cb_poll_status()[0] == 0
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_fewer_tokens_than_alternatives(dtype):
+    for V in (1, 7, 19):
+        cb = context(vocab=V)
+        x, tok = _logits(4, V, dtype, V)
+        got = cb.cb_logprobs(x, tok, top_k=20)
+        assert (got["top_ids"][:, V:] == -1).all() and (got["top_logprobs"][:, V:] == -math.inf).all()
+        _check({k: v[:, :V] if k.startswith("top") else v for k, v in got.items()}, x, tok, V, V)
+
+
 def test_far_apart_and_large_logits():
     V = 4096
     cb = context(vocab=V)

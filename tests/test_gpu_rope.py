@@ -110,6 +110,12 @@ def test_append_leaves_sequences_alone_that_do_not_fit():
     assert (out[5:9] == 7).all() and int(changed.sum()) == 3 + 2 + 2
     out, changed = run(_lib.CB_ERR_INVALID_ARG, ok, rope_table(6, 16))             # the last row's position is 6
     assert (out[10] == 7).all() and int(changed.sum()) == 10 and not (out[9] == 7).all()
+    was = c.d_start
+    for start, left in (([0, 3, 5, 9, 50], range(9, 11)), ([-3, 3, 5, 9, 11], range(3))):        # a range that is not of these rows
+        c.d_start = cuda(start)
+        out, changed = run(_lib.CB_ERR_INVALID_ARG, ok)
+        assert (out[list(left)] == 7).all() and int(changed.sum()) == 11 - len(left)
+    c.d_start = was
     bt = c.block_table.clone()
     bt[0, 0], bt[2, 0] = c.num_pages, -5
     out, changed = run(_lib.CB_ERR_INVALID_ARG, ok, None, bt)

@@ -23,23 +23,48 @@ struct RopeParams {
     uint32_t* status;
 };
 
-__device__ __forceinline__ void unpack8(const uint4& u, float* x) {
+// Two fp32 values in one 64-bit register pair, for the packed arithmetic of sm_100.
+__device__ __forceinline__ uint64_t f2_pack(float lo, float hi) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ void f2_unpack(uint64_t v, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
+__device__ __forceinline__ uint64_t f2_fma(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ uint64_t f2_mul(uint64_t a, uint64_t b) {
+    uint64_t d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ uint64_t f2_neg(uint64_t a) { return a ^ 0x8000000080000000ull; }
+__device__ __forceinline__ uint64_t f2_swap(uint64_t a) { return a >> 32 | a << 32; }
+
+// Eight elements as four pairs of neighbours.
+__device__ __forceinline__ void unpack8(const uint4& u, uint64_t* x) {
     const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) { x[2 * i] = __uint_as_float(w[i] << 16); x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u); }
+    for (int i = 0; i < 4; ++i) x[i] = f2_pack(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xFFFF0000u));
 }
-__device__ __forceinline__ uint4 pack8(const float* x) {
+__device__ __forceinline__ uint4 pack8(const uint64_t* x) {
     uint32_t w[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const __nv_bfloat162 p = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+        float lo, hi;
+        f2_unpack(x[i], lo, hi);
+        const __nv_bfloat162 p = __floats2bfloat162_rn(lo, hi);
         w[i] = *reinterpret_cast<const uint32_t*>(&p);
     }
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-template <int D, bool TREE, int U>
-__global__ void __launch_bounds__(32 * kRopeWarps) cb_rope_kernel(const RopeParams p) {
+// INTER: pairs are neighbours.  Of the kernels with four groups a warp, which have the most registers, five blocks an SM for trees and six for chunks:
+// 16,384 tree rows of 64/8 heads 119 us with five and 134 with six, 8,192 rows of a chunk 72 and 68.
+template <int D, bool TREE, bool INTER, int U>
+__global__ void __launch_bounds__(32 * kRopeWarps, U == 4 ? (TREE ? 5 : 6) : 4) cb_rope_kernel(const RopeParams p) {
     CB_PDL_ENTRY();
     constexpr int LPH = D / 16, HPW = 32 / LPH;               // lanes per head, heads that a warp holds side by side
     const int lane = threadIdx.x & 31, sub = lane % LPH;
@@ -50,7 +75,7 @@ __global__ void __launch_bounds__(32 * kRopeWarps) cb_rope_kernel(const RopePara
     const int R = p.rope ? p.R : 0;
     const bool turned = sub < R / 16;                         // both pieces are, or neither
     int ca = 2 * sub, cb = 2 * sub + 1;
-    if (turned && !p.interleaved) { ca = sub; cb = sub + R / 16; }   // (the lanes behind these hold what lies behind R)
+    if (turned && !INTER) { ca = sub; cb = sub + R / 16; }   // (the lanes behind these hold what lies behind R)
     // A row's heads in one count: its queries, then its keys, then its values.
     auto is_q = [&](int u) { return slot0 + u * HPW < p.Hq; };
     auto is_qk = [&](int u) { return slot0 + u * HPW < p.Hq + p.Hkv; };
@@ -101,12 +126,20 @@ __global__ void __launch_bounds__(32 * kRopeWarps) cb_rope_kernel(const RopePara
         }
         kv_row = (size_t)page * p.P + ((uint32_t)pos - at * (uint32_t)p.P);
     }
-    float c[8], s[8];                                         // the same for every head of the row
+    // The angles, the same for every head of the row.  Halves: cosines and sines of this lane's eight pairs (i, i + R / 2), two pairs to a register.
+    // Neighbours: a pair (x, y) and its swap (y, x) times (c, c) and (-s, s).
+    uint64_t c[8], s[8];
     if (turned && !dead) {
+        float fc[8], fs[8];
         const float4* rc = reinterpret_cast<const float4*>(p.rope + pos * R + 8 * sub);
         const float4* rs = reinterpret_cast<const float4*>(p.rope + pos * R + R / 2 + 8 * sub);
-        *reinterpret_cast<float4*>(c) = rc[0]; *reinterpret_cast<float4*>(c + 4) = rc[1];
-        *reinterpret_cast<float4*>(s) = rs[0]; *reinterpret_cast<float4*>(s + 4) = rs[1];
+        *reinterpret_cast<float4*>(fc) = rc[0]; *reinterpret_cast<float4*>(fc + 4) = rc[1];
+        *reinterpret_cast<float4*>(fs) = rs[0]; *reinterpret_cast<float4*>(fs + 4) = rs[1];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (INTER) { c[i] = f2_pack(fc[i], fc[i]); s[i] = f2_pack(-fs[i], fs[i]); }
+            else if (i < 4) { c[i] = f2_pack(fc[2 * i], fc[2 * i + 1]); s[i] = f2_pack(fs[2 * i], fs[2 * i + 1]); }
+        }
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -115,39 +148,41 @@ __global__ void __launch_bounds__(32 * kRopeWarps) cb_rope_kernel(const RopePara
             ua[u] = ub[u] = make_uint4(0, 0, 0, 0);
         } else {
             const __nv_bfloat16* w = is_q(u) ? p.q_norm : p.k_norm;
-            float a[8], b[8];
+            uint64_t a[4], b[4];
             unpack8(ua[u], a);
             unpack8(ub[u], b);
             if (p.q_norm || p.k_norm) {                       // all lanes: the sum is by shuffles
-                float ss = 0.f;
+                uint64_t s2 = f2_mul(a[0], a[0]);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) ss = fmaf(a[i], a[i], fmaf(b[i], b[i], ss));
+                for (int i = 1; i < 4; ++i) s2 = f2_fma(a[i], a[i], s2);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s2 = f2_fma(b[i], b[i], s2);
+                float ss, hi;
+                f2_unpack(s2, ss, hi);
+                ss += hi;
 #pragma unroll
                 for (int o = 1; o < LPH; o <<= 1) ss += __shfl_xor_sync(CB_FULL, ss, o);
                 if (is_qk(u) && w) {
                     const float inv = rsqrtf(ss * (1.0f / D) + p.eps);
-                    float wa[8], wb[8];
+                    const uint64_t inv2 = f2_pack(inv, inv);
+                    uint64_t wa[4], wb[4];
                     unpack8(*reinterpret_cast<const uint4*>(w + ca * 8), wa);
                     unpack8(*reinterpret_cast<const uint4*>(w + cb * 8), wb);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) { a[i] *= inv * wa[i]; b[i] *= inv * wb[i]; }
+                    for (int i = 0; i < 4; ++i) { a[i] = f2_mul(a[i], f2_mul(inv2, wa[i])); b[i] = f2_mul(b[i], f2_mul(inv2, wb[i])); }
                 }
             }
             if (is_qk(u)) {
                 if (turned) {
-                    if (p.interleaved) {
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const float a0 = a[2 * i], a1 = a[2 * i + 1], b0 = b[2 * i], b1 = b[2 * i + 1];
-                            a[2 * i] = a0 * c[i] - a1 * s[i]; a[2 * i + 1] = a1 * c[i] + a0 * s[i];
-                            b[2 * i] = b0 * c[4 + i] - b1 * s[4 + i]; b[2 * i + 1] = b1 * c[4 + i] + b0 * s[4 + i];
-                        }
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            const float x = a[i], y = b[i];
-                            a[i] = x * c[i] - y * s[i];
-                            b[i] = y * c[i] + x * s[i];
+                    for (int i = 0; i < 4; ++i) {
+                        const uint64_t x = a[i], y = b[i];
+                        if (INTER) {
+                            a[i] = f2_fma(f2_swap(x), s[i], f2_mul(x, c[i]));
+                            b[i] = f2_fma(f2_swap(y), s[4 + i], f2_mul(y, c[4 + i]));
+                        } else {
+                            a[i] = f2_fma(f2_neg(y), s[i], f2_mul(x, c[i]));
+                            b[i] = f2_fma(x, s[i], f2_mul(y, c[i]));
                         }
                     }
                 }
@@ -191,14 +226,15 @@ cb_status launch_rope_of(RopeParams p, int D, cudaStream_t st) {
     p.parts = (p.Hq + 2 * p.Hkv + per_warp - 1) / per_warp;
     const long long blocks = ((long long)p.n_rows * p.parts + kRopeWarps - 1) / kRopeWarps;
     if (blocks * kRopeWarps > 0x7FFFFFFFll) return CB_ERR_UNSUPPORTED;
-    auto kernel = D == 128 ? cb_rope_kernel<128, TREE, U> : cb_rope_kernel<64, TREE, U>;
+    auto kernel = p.interleaved ? (D == 128 ? cb_rope_kernel<128, TREE, true, U> : cb_rope_kernel<64, TREE, true, U>)
+                                : (D == 128 ? cb_rope_kernel<128, TREE, false, U> : cb_rope_kernel<64, TREE, false, U>);
     CB_CUDA(cb_launch_pdl(kernel, dim3((unsigned)blocks), dim3(32 * kRopeWarps), 0, st, p));
     cb_count_launch(1);
     return CB_OK;
 }
 // Groups of heads per warp: one where warps are few, since a call then takes what one of them takes; more where there are plenty, since what
 // belongs to the row (its sequence, position, page, angles) is found once for all of them and their loads are under way together.  us with 1, 2, 4:
-// 8,192 rows of 64/8 heads 87.8, 75.2, 68.1; 16,384 tree rows of them 158, 125, 123; 4,096 of 32/8 26.4, 23.5, 22.4; 2,048 tree rows of 32/8 13.7, 11.3, 13.3.
+// 8,192 rows of 64/8 heads 87.8, 75.2, 68.1; 16,384 tree rows of them 158, 125, 119; 4,096 of 32/8 26.4, 23.5, 22.4; 2,048 tree rows of 32/8 13.7, 11.3, 13.3.
 template <bool TREE>
 cb_status launch_rope(const RopeParams& p, int D, cudaStream_t st) {
     const int per_warp = 32 / (D / 16);

@@ -57,7 +57,7 @@ enum { CB_DTYPE_F32 = 0, CB_DTYPE_BF16 = 1 };
 /* cb_config.flags */
 enum {
     CB_FLAG_NO_FOLLOWER_REFRESH = 1u, /* re-inserting a stored follower leaves its recency unchanged     */
-    CB_FLAG_ATTN_CUDA_CORES = 2u,     /* run tree attention on the plain CUDA-core kernel (debug aid)    */
+    CB_FLAG_ATTN_CUDA_CORES = 2u,     /* run tree and chunk attention on plain CUDA-core kernels (debug aid) */
     CB_FLAG_ATTN_CTA_PAIRS = 4u       /* tree attention of multi-row-tile launches (head_dim 128) as pairs of
                                          CTAs issuing 2-CTA tensor-core products; measured slower than the
                                          default on the configurations benchmarked, kept as an alternative */

@@ -118,6 +118,25 @@ __global__ void __launch_bounds__(kThreads, 1) cb_chunk_tc_kernel(const CbChunkP
         if (lane < 16) s_pair[lane] = 0;
     }
     CB_PDL_ENTRY();
+    // What the first copy waits for is asked for before the barrier and lies in L1 when it is wanted: the lengths that the schedule reads first, and,
+    // where a unit's CTAs are known, the block table's entries of this CTA's first tile if the sequence is as long as the caller's bound.
+    const int unit = p.cs == 0 ? 0 : (p.cs == 1 ? cta : (int)__umulhi((uint32_t)cta, p.cs_inv)), seq_b = p.Hkv == 1 ? unit : (int)__umulhi((uint32_t)unit, p.hkv_inv);
+    if (warp == 2) {
+        const int b = p.cs > 0 ? seq_b : lane;
+        if (b < p.B) {
+            uint32_t x;
+            asm volatile("ld.global.ca.u32 %0, [%1];" : "=r"(x) : "l"(p.q_start + b) : "memory");
+            asm volatile("ld.global.ca.u32 %0, [%1];" : "=r"(x) : "l"(p.q_start + b + 1) : "memory");
+            asm volatile("ld.global.ca.u32 %0, [%1];" : "=r"(x) : "l"(p.ctx_len + b) : "memory");
+        }
+    } else if ((warp == 0 || warp == 3) && p.cs > 0 && lane == 0) {
+        const int tiles = (p.max_keys + CB_KT - 1) / CB_KT, n = min(p.cs, tiles);
+        const long long at = cb_quot((long long)(tiles * min(cta - unit * p.cs, n - 1)), n) * (CB_KT / 16);
+        if (at < p.max_pages) {
+            uint32_t x;
+            asm volatile("ld.global.ca.u32 %0, [%1];" : "=r"(x) : "l"(p.block_table + (size_t)seq_b * p.max_pages + at) : "memory");
+        }
+    }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -278,8 +297,8 @@ __global__ void __launch_bounds__(kThreads, 1) cb_chunk_tc_kernel(const CbChunkP
             if (p.cs > 0) {
                 CbChunkShape s;
                 int np = 0;
-                const int unit = p.cs == 1 ? cta : (int)__umulhi((uint32_t)cta, p.cs_inv), b = p.Hkv == 1 ? unit : (int)__umulhi((uint32_t)unit, p.hkv_inv), cf = unit * p.cs;
-                const bool has = cb_chunk_share(p, b, unit - b * p.Hkv, cta - cf, &x, &s, &np);
+                const int cf = unit * p.cs;
+                const bool has = cb_chunk_share(p, seq_b, unit - seq_b * p.Hkv, cta - cf, &x, &s, &np);
                 error = s.error;
                 if (lane == 0 && has) {
                     volatile ChunkUnit* u = &s_units[0];
@@ -664,8 +683,8 @@ __global__ void __launch_bounds__(kThreads, 1) cb_chunk_tc_kernel(const CbChunkP
                                 for (int q = 0; q < 4; ++q) v[q] = vn[q];
                             }
                         } else {
-                            // Many parts: two at a time are fetched, with their references, before either is used (one after the other, with what
-                            // CTA 5 of 6 left at batch 1, the last to come spent 14 k cycles here).
+                            // Many parts: two at a time are fetched, with their references, before either is used (one after the other, the last
+                            // to come of six spent 14 k cycles here).
                             auto part2 = [&](int k, const float* pp, float2* ml) { *ml = k >= np ? make_float2(-INFINITY, 0.f) : (pp == own ? make_float2(x_m, x_l) : load_ml(pp)); };
 #pragma unroll 1
                             for (int k = 0; k < np; k += 4) {
@@ -719,11 +738,7 @@ __global__ void __launch_bounds__(kThreads, 1) cb_chunk_tc_kernel(const CbChunkP
                 if (lane == 0) mbar_arrive(bar_sums);
                 if (!(ok = mbar_wait(bar_sums, 1, s_abort, p.status))) break;
                 volatile int* const s_last = reinterpret_cast<volatile int*>(sgen + C::OFF_X);
-                if (sw == 0 && lane == 0) {
-                    __threadfence();
-                    *s_last = atom_add_acq_rel(p.part_ticket + u->ticket, 1u) == (uint32_t)(np - 1);
-                    __threadfence();
-                }
+                if (sw == 0 && lane == 0) *s_last = atom_add_acq_rel(p.part_ticket + u->ticket, 1u) == (uint32_t)(np - 1);   // releases what it saw stored
                 if (lane == 0) mbar_arrive(bar_ofree(0));     // (nobody waits there for the accumulator of an only unit)
                 if (!(ok = mbar_wait(bar_ofree(0), 0, s_abort, p.status))) break;
                 if (*s_last) {

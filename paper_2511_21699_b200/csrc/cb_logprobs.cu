@@ -4,11 +4,12 @@
 // maximum when one comes.  The threads' (m, s, t) then go on the row's maximum M: log Z = M + log s, the token's log probability is
 // (x - M) - log s, the entropy log s - t / s (two terms that are not negative, so nothing cancels).
 //
-// The alternatives need no second pass over the row.  Elements are ordered by value, equal ones by falling id (a 64-bit key).  Every
-// thread knows its largest element, and 32 groups of threads each theirs; at least K elements reach the K-th largest of those 32, and only the
-// few threads whose own largest does (some 30 for K = 20) can hold any.  Their elements are looked at once more (they are in L2), what reaches the
-// bound is listed, little more than K elements as a rule, and the list is ranked by counting.  (Ranking the 256 threads' keys, and reading
-// their largest elements again to find the ids, made this part 12 k cycles long beside the 11 k of a row of 32 k bf16 logits.)
+// The alternatives need no second pass over the row.  Every thread notes the largest element of each of its steps, which it computes anyway.  At least K
+// elements reach the K-th largest of 32 groups of threads' largest elements, and steps whose largest does are few (some 30 for K = 20); only
+// those 64 bytes each are looked at once more, what reaches the bound is listed as a key (value, then falling id), little more than K elements as a rule,
+// and the list is ranked by counting.  Where too many are as large as the bound (a constant row, or fewer than K tokens that are not forbidden), the list
+// has those above it, and the lowest ids among the equal ones follow in order.  (Keys of all threads ranked, their elements all looked at again:
+// 12 k cycles beside the 11 k of a row of 32 k bf16 logits.)
 //
 // A row is one CTA's, or, where that leaves SMs idle, a cluster's, whose CTAs take equal parts of it and hand their sums and their K best
 // to the first one through distributed shared memory.
@@ -22,7 +23,8 @@ constexpr int kThreads = 256, kWarps = kThreads / 32;         // (512 threads a 
 constexpr int kUnroll = 4;                                    // 16-byte pieces of a thread at a time
 constexpr int kStep = kThreads * kUnroll;                     // and of the CTA
 constexpr int kGroup = kThreads / 32;                         // threads of one of 32 groups
-constexpr int kCand = 1024;                                   // elements listed; more than that are taken one after the other
+constexpr int kCand = 1024;                                   // elements listed at most
+constexpr int kSlots = 32, kBlocks = 1024;                    // noted maxima of a thread; (thread, slot) blocks looked at again at most
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 // The same place in another CTA of the cluster, and loads from there.
@@ -204,9 +206,10 @@ __global__ void __launch_bounds__(kThreads, 4) cb_logprobs_kernel(const LogprobP
     CB_PDL_ENTRY();
     constexpr int E = Row<BF16>::E;
     __shared__ Stat s_stat[kWarps], s_all;
-    __shared__ unsigned long long s_key[32], s_cand[TOP ? kCand : 1], s_best[kWarps], s_top[TOP ? CB_MAX_TOP : 1];
-    __shared__ int s_list[TOP ? kThreads : 1], s_lists, s_count;
-    __shared__ uint4 s_max[TOP ? kUnroll : 1][TOP ? kThreads : 1];          // every thread's step with its largest element
+    __shared__ unsigned long long s_cand[TOP ? kCand : 1], s_best[kWarps], s_top[TOP ? CB_MAX_TOP : 1];
+    __shared__ float s_hi[TOP ? kSlots : 1][TOP ? kThreads : 1], s_group[32];
+    __shared__ unsigned short s_block[TOP ? kBlocks : 1];
+    __shared__ int s_blocks, s_count, s_equal[kWarps];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int i = blockIdx.x / p.cs, part = blockIdx.x - i * p.cs;          // the row's output, and which part of the row is this CTA's
     int row = i, tok = p.tokens ? p.tokens[i] : 0;
@@ -237,10 +240,13 @@ __global__ void __launch_bounds__(kThreads, 4) cb_logprobs_kernel(const LogprobP
 
     float ref = -INFINITY;                                    // the thread's running maximum
     uint64_t s2 = 0, t2 = 0;                                  // two sums each
-    int best = 0;                                             // step at which the maximum came
+    // alternatives: the largest element of every so many steps
+    const int steps = (end - begin + kStep - 1) / kStep, per_slot = (steps + kSlots - 1) / kSlots;
+    int slots = 0, in_slot = 0;
+    float slot_hi = -INFINITY;
     Block<BF16> cur, next;                                    // (three steps in shared memory, by bulk copies, were no faster than one ahead in registers)
     load_block(cur, r, begin + tid, end);
-    for (int k0 = begin + tid, step = 0; k0 < end; k0 += kStep, ++step) {
+    for (int k0 = begin + tid; k0 < end; k0 += kStep) {
         load_block(next, r, k0 + kStep, end);
         float hi, lo;
         extremes(cur, hi, lo);
@@ -254,14 +260,10 @@ __global__ void __launch_bounds__(kThreads, 4) cb_logprobs_kernel(const LogprobP
                 s2 = f2_pack(s0 * w, s1 * w);
             }
             ref = hi;
-            if constexpr (TOP) {
-                best = step;
-#pragma unroll
-                for (int q = 0; q < kUnroll; ++q) s_max[q][tid] = cur.u[q];
-            }
-        } else if (TOP && step == 0) {                        // nothing but -inf
-#pragma unroll
-            for (int q = 0; q < kUnroll; ++q) s_max[q][tid] = cur.u[q];
+        }
+        if constexpr (TOP) {
+            slot_hi = fmaxf(slot_hi, hi);
+            if (++in_slot == per_slot) { s_hi[slots++][tid] = slot_hi; slot_hi = -INFINITY; in_slot = 0; }
         }
         const float base = ref == -INFINITY ? 0.f : ref;
         if (lo == -INFINITY) add_block<BF16, true>(cur, base, s2, t2);
@@ -286,26 +288,13 @@ __global__ void __launch_bounds__(kThreads, 4) cb_logprobs_kernel(const LogprobP
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) a = join(a, {__shfl_xor_sync(CB_FULL, a.m, o), __shfl_xor_sync(CB_FULL, a.s, o), __shfl_xor_sync(CB_FULL, a.t, o)});
     if (lane == 0) s_stat[warp] = a;
-    unsigned long long mine = 0;
     if constexpr (TOP) {
-        // this thread's largest element, the lowest id among equal ones, and its group's
-        const int k0 = begin + tid + best * kStep;
+        if (in_slot) s_hi[slots++][tid] = slot_hi;
+        float group = ref;
 #pragma unroll
-        for (int q = kUnroll - 1; q >= 0; --q) {
-            if (k0 + q * kThreads >= end) continue;
-            float x[E];
-            unpack<BF16>(s_max[q][tid], x);
-            int at = -1;
-#pragma unroll
-            for (int j = E - 1; j >= 0; --j)
-                if (x[j] == ref) at = j;
-            if (at >= 0) mine = key_of(ref, r.id(k0 + q * kThreads, at));
-        }
-        unsigned long long group = mine;
-#pragma unroll
-        for (int o = 1; o < kGroup; o <<= 1) group = max(group, __shfl_xor_sync(CB_FULL, group, o));
-        if (lane % kGroup == 0) s_key[tid / kGroup] = group;
-        if (tid == 0) { s_count = 0; s_lists = 0; }
+        for (int o = 1; o < kGroup; o <<= 1) group = fmaxf(group, __shfl_xor_sync(CB_FULL, group, o));
+        if (lane % kGroup == 0) s_group[tid / kGroup] = group;
+        if (tid == 0) s_blocks = s_count = 0;
     }
     __syncthreads();
     if (warp == 0) {                                          // the CTA's sums; only this warp writes any result
@@ -315,89 +304,141 @@ __global__ void __launch_bounds__(kThreads, 4) cb_logprobs_kernel(const LogprobP
         if (lane == 0) s_all = a;
     }
     if constexpr (TOP) {
-        // the bound, in every warp, and the threads that reach it
-        const unsigned long long key = s_key[lane];
+        // the bound, in every warp: the K-th largest of the groups' (equal ones by number)
+        const float mine = s_group[lane];
         int rank = 0;
 #pragma unroll
-        for (int o = 0; o < 32; ++o) rank += s_key[o] > key;
-        const uint32_t who = __ballot_sync(CB_FULL, key != 0 && rank == p.K - 1);
-        const unsigned long long bound = who ? __shfl_sync(CB_FULL, key, __ffs(who) - 1) : 0;    // 0: fewer than K groups have any
-        const float least = bound ? value_of(bound) : -INFINITY;
-        if (mine != 0 && mine >= bound) s_list[atomicAdd(&s_lists, 1)] = tid;
-        __syncthreads();
-        const int lists = s_lists;
-        auto list = [&](unsigned long long k) {
-            if (k < bound) return;
-            const int at = atomicAdd(&s_count, 1);
-            if (at < kCand) s_cand[at] = k;
-        };
-        // all their pieces dealt to the threads, four loads at a time
-        const int rounds = (end - begin + kThreads - 1) / kThreads, all = lists * rounds;
-        const float inv_rounds = 1.0f / (float)max(rounds, 1);
-        auto div_rounds = [&](int w) {                        // w / rounds; the product is off by one at most
-            int l = (int)((float)w * inv_rounds);
-            if (l * rounds > w) --l;
-            else if ((l + 1) * rounds <= w) ++l;
-            return l;
-        };
-        for (int w0 = tid; w0 < all; w0 += 4 * kThreads) {
-            int at[4];
-            uint4 u[4];
+        for (int o = 0; o < 32; ++o) rank += s_group[o] > mine || (s_group[o] == mine && o < lane);
+        const float bound = __shfl_sync(CB_FULL, mine, __ffs(__ballot_sync(CB_FULL, rank == p.K - 1)) - 1);
+        // Lists the elements that reach the bound, or lie above it, as keys; false: there are too many.
+        auto collect = [&](bool above) {
+            auto in = [&](float x) { return above ? x > bound : x >= bound; };
+            auto list = [&](unsigned long long k) {
+                const int at = atomicAdd(&s_count, 1);
+                if (at < kCand) s_cand[at] = k;
+            };
+            for (int k = 0; k < slots; ++k)
+                if (in(s_hi[k][tid])) {
+                    const int at = atomicAdd(&s_blocks, 1);
+                    if (at < kBlocks) s_block[at] = (unsigned short)(k * kThreads + tid);
+                }
+            __syncthreads();
+            const int blocks = s_blocks;
+            if (blocks > kBlocks) return false;
+            // all their pieces dealt to the threads, four loads at a time
+            const int pieces = per_slot * kUnroll, all = blocks * pieces;
+            for (int w0 = tid; w0 < all; w0 += 4 * kThreads) {
+                int at[4];
+                uint4 u[4];
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int w = w0 + q * kThreads, l = div_rounds(w);
-                at[q] = w < all ? begin + s_list[l] + (w - l * rounds) * kThreads : end;
-                if (at[q] < end) u[q] = r.piece(at[q]);
+                for (int q = 0; q < 4; ++q) {
+                    const int w = w0 + q * kThreads, b = per_slot == 1 ? w / kUnroll : w / pieces, r4 = w - b * pieces;
+                    at[q] = end;
+                    if (w < all) {
+                        const int block = s_block[b];
+                        at[q] = begin + (block / kThreads * per_slot + r4 / kUnroll) * kStep + r4 % kUnroll * kThreads + block % kThreads;
+                    }
+                    if (at[q] < end) u[q] = r.piece(at[q]);
+                }
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    if (at[q] >= end) continue;
+                    float x[E], hi = -INFINITY;
+                    unpack<BF16>(u[q], x);
+#pragma unroll
+                    for (int j = 0; j < E; ++j) hi = fmaxf(hi, x[j]);
+                    if (!in(hi)) continue;                    // most pieces
+#pragma unroll
+                    for (int j = 0; j < E; ++j)
+                        if (in(x[j])) list(key_of(x[j], r.id(at[q], j)));
+                }
             }
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                if (at[q] >= end) continue;
-                float x[E], hi = -INFINITY;
-                unpack<BF16>(u[q], x);
-#pragma unroll
-                for (int j = 0; j < E; ++j) hi = fmaxf(hi, x[j]);
-                if (hi < least) continue;                     // most pieces
-#pragma unroll
-                for (int j = 0; j < E; ++j) list(key_of(x[j], r.id(at[q], j)));
-            }
+            if (my_odd >= 0 && in(x_odd)) list(key_of(x_odd, my_odd));
+            __syncthreads();
+            return s_count <= kCand;
+        };
+        bool listed = collect(false), equals = false;
+        if (!listed) {
+            __syncthreads();
+            if (tid == 0) s_blocks = s_count = 0;
+            __syncthreads();
+            listed = collect(true);
+            equals = true;
         }
-        const unsigned long long odd_key = my_odd >= 0 ? key_of(x_odd, my_odd) : 0;
-        if (my_odd >= 0) list(odd_key);
-        __syncthreads();
-        const int count = s_count, found = min(count, p.K);
-        if (count <= kCand) {
+        int found = 0;
+        if (listed) {
+            const int count = s_count;
+            found = min(count, p.K);
             for (int c = tid; c < count; c += kThreads) {
                 const unsigned long long k = s_cand[c];
                 int at = 0;
                 for (int o = 0; o < count; ++o) at += s_cand[o] > k;
                 if (at < p.K) s_top[at] = k;
             }
-        } else {
-            // a few threads' elements make up much of what is large (a sorted row, say): one after the other
-            unsigned long long last = ~0ull;
-            for (int at = 0; at < found; ++at) {
-                unsigned long long k1 = odd_key < last ? odd_key : 0;
-                for (int l = warp; l < lists; l += kWarps)
-                    for (int k = begin + s_list[l] + lane * kThreads; k < end; k += 32 * kThreads) {
-                        float x[E];
-                        unpack<BF16>(r.piece(k), x);
+            // the bound's equals in the order of their ids: what lies before the pieces, the pieces, 256 at a time, what lies behind them
+            for (int k0 = begin - kThreads; equals && found < p.K && k0 < end + kThreads; k0 += kThreads) {
+                const bool head = k0 < begin, tail = k0 >= end;
+                const int k = k0 + tid;
+                uint32_t equal = 0;                           // which of this thread's elements
+                if (head || tail) {
+                    const int o = head ? tid : r.head + tid;
+                    if (part == 0 && o < (head ? r.head : r.head + r.tail)) equal = r.at(r.odd(o)) == bound;
+                } else if (k < end) {
+                    float x[E];
+                    unpack<BF16>(r.piece(k), x);
 #pragma unroll
-                        for (int j = 0; j < E; ++j) {
-                            const unsigned long long c = key_of(x[j], r.id(k, j));
-                            if (c < last && c > k1) k1 = c;
-                        }
+                    for (int j = 0; j < E; ++j) equal |= (uint32_t)(x[j] == bound) << j;
+                }
+                int before = __popc(equal);
+#pragma unroll
+                for (int o = 1; o < 32; o <<= 1) {
+                    const int t = __shfl_up_sync(CB_FULL, before, o);
+                    if (lane >= o) before += t;
+                }
+                if (lane == 31) s_equal[warp] = before;
+                before -= __popc(equal);
+                __syncthreads();
+                int total = 0;
+                for (int w = 0; w < kWarps; ++w) {
+                    if (w < warp) before += s_equal[w];
+                    total += s_equal[w];
+                }
+                for (int at = found + before; equal != 0 && at < p.K; ++at) {
+                    const int j = __ffs(equal) - 1;
+                    equal &= equal - 1;
+                    s_top[at] = key_of(bound, head ? r.odd(tid) : (tail ? r.odd(r.head + tid) : r.id(k, j)));
+                }
+                found = min(found + total, p.K);
+                __syncthreads();
+            }
+        } else {
+            // thousands above the bound too (a few threads' elements make up what is large, as in a sorted row): one after the other
+            unsigned long long last = ~0ull;
+            while (found < p.K) {
+                unsigned long long k1 = 0;
+                if (my_odd >= 0 && x_odd == x_odd && key_of(x_odd, my_odd) < last) k1 = key_of(x_odd, my_odd);
+                for (int k = begin + tid; k < end; k += kThreads) {
+                    float x[E];
+                    unpack<BF16>(r.piece(k), x);
+#pragma unroll
+                    for (int j = 0; j < E; ++j) {
+                        const unsigned long long c = x[j] == x[j] ? key_of(x[j], r.id(k, j)) : 0;
+                        if (c < last && c > k1) k1 = c;
                     }
+                }
 #pragma unroll
                 for (int o = 16; o > 0; o >>= 1) k1 = max(k1, __shfl_xor_sync(CB_FULL, k1, o));
                 if (lane == 0) s_best[warp] = k1;
                 __syncthreads();
                 for (int w = 0; w < kWarps; ++w) k1 = max(k1, s_best[w]);
-                last = k1;
-                if (tid == 0) s_top[at] = k1;
+                if (tid == 0) s_top[found] = k1;
                 __syncthreads();
+                if (k1 == 0) break;
+                last = k1;
+                ++found;
             }
         }
-        if (tid >= found && tid < p.K) s_top[tid] = 0;
+        if (tid >= found && tid < p.K) s_top[tid] = 0;        // (places that nobody has written)
     }
     if (p.cs > 1) {
         // The first CTA reads what the others have; they stay until it has.

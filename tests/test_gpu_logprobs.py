@@ -135,6 +135,32 @@ def test_fewer_tokens_than_alternatives(dtype):
         _check({k: v[:, :V] if k.startswith("top") else v for k, v in got.items()}, x, tok, V, V)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V,pad", [(5000, 0), (32003, 3), (100001, 1), (700001, 0)])
+def test_more_equals_than_places(V, pad, dtype):
+    """Rows in which thousands are as large as the K-th: constant but for a few, a handful of allowed tokens (fewer than K, in every part of the row),
+    steps of equal values, and rows whose views start at odd places."""
+    cb = context(vocab=V)
+    x = torch.zeros(7, V + pad, device="cuda")[:, pad:]
+    g = torch.Generator(device="cuda").manual_seed(V)
+    at = torch.randperm(V, generator=g, device="cuda")
+    x[0, at[:3]] = 2.0
+    x[1] = -math.inf
+    x[1, at[:11]] = torch.randn(11, generator=g, device="cuda")
+    x[2] = -math.inf
+    x[2, torch.tensor([0, V - 1, V // 2], device="cuda")] = 1.0    # the outermost ids
+    x[3] = torch.arange(V, device="cuda") // (V // 3)
+    x[4, :] = -1.0
+    x[4, V - 2:] = 0.0
+    x[5] = -torch.ones(V, device="cuda")
+    x[5, at[:500]] = 3.0
+    x[6] = torch.where(torch.arange(V, device="cuda") % 2 == 0, 0.5, -math.inf)
+    x = x.to(dtype)
+    tok = cuda([int(at[0])] * 2 + [0, 5, 7, int(at[1]), 2])
+    for top in (1, 12, 20, 32):
+        _check(cb.cb_logprobs(x, tok, top_k=top), x, tok, top, top)
+
+
 def test_far_apart_and_large_logits():
     V = 4096
     cb = context(vocab=V)

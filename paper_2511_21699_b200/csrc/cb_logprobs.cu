@@ -493,9 +493,9 @@ __global__ void __launch_bounds__(kThreads, 4) cb_logprobs_kernel(const LogprobP
 
 // CTAs per row.  A cluster costs a launch some 0.3 us and every row the hand-over; it pays where rows alone leave SMs without work, and, with
 // up to four CTAs an SM, where a row is so long that its CTA ends well after the rest.  Measured, us with 1, 2, 4, 8 CTAs a row:
-//   9 rows of 128 k fp32 10.6, 7.6, 5.6, 4.6;  40 of 128 k bf16 12.4, 8.9, 7.0, 7.8;  75 of 50 k fp32 10.4, 8.3, 7.9, 9.7
-//   150 of 128 k bf16 15.1, 16.6, 14.8, 16.9;  300 of 128 k bf16 27.6, 21.8, 23.3, 28.4;  300 of 50 k fp32 14.7, 18.4, 20.1, 24.7
-//   150 of 128 k fp32 with 20 alternatives 30.6, 27.7, 31.7, 38.3;  9 of 32 k bf16 with five 6.4, 7.1, 6.8, 6.7;  600 of 128 k 34.8, 35.0, 39.9, 52.8
+//   9 rows of 128 k fp32 10.5, 7.5, 5.5, 4.4;  40 of 128 k bf16 12.7, 9.0, 7.0, 7.8;  75 of 50 k fp32 10.7, 8.3, 7.7, 9.8
+//   150 of 128 k bf16 15.0, 16.5, 14.7, 16.8;  300 of 128 k bf16 27.5, 21.8, 23.2, 28.4;  300 of 50 k fp32 14.7, 18.5, 20.0, 24.6;  600 of 128 k 34.6, 35.0, 39.9, 52.7
+//   with 20 alternatives 9 of 128 k bf16 14.4, 11.1, 8.8, 8.4;  40 16.1, 12.4, 11.5, 14.0;  150 of fp32 27.9, 24.8, 29.8, 37.0;  with five 9 of 32 k 6.6, 7.1, 6.5, 6.4
 int pick_cluster(long long rows, int V, int K, int num_sms) {
     int cs = 1;
     if (V < 48000) return cs;

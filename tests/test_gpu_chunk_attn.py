@@ -115,20 +115,24 @@ def test_long_chunk_on_a_long_context(d):
 
 
 @pytest.mark.parametrize("flags", [0, 2])
-def test_scores_far_apart_and_rising(flags):
-    """A row's maximum comes late, by far: every reference is passed again and again."""
-    d, n, ctx = 64, 70, 900
-    c = Paged([n], [ctx], 1, d)
-    step = torch.linspace(0.1, 30, ctx + n, device="cuda")
-    at = c.slots(0, 0, ctx + n)
-    c.k.view(-1, 1, d)[at, 0] = step[:, None].to(BF).expand(-1, d).contiguous()
-    q = torch.ones(n, 2, d, device="cuda", dtype=BF)
+@pytest.mark.parametrize("d,hkv,new,ctx", [(64, 1, [70], [900]), (128, 1, [70], [900]), (64, 2, [1, 1, 1], [1500, 300, 129]), (128, 4, [1, 1], [2000, 700]),
+                                           (64, 3, [300, 1, 200], [0, 800, 130]), (128, 2, [257, 33], [128, 500])])
+def test_scores_far_apart_and_rising(d, hkv, new, ctx, flags):
+    """A row's maximum comes late, by far: every reference is passed again and again.  Two row tiles, single tokens (shared by CTAs, or two heads at a
+    time), and both mixed."""
+    c = Paged(new, ctx, hkv, d)
+    for b in range(len(new)):
+        at = c.slots(b, 0, ctx[b] + new[b])
+        step = torch.linspace(0.1, 30, len(at), device="cuda")
+        c.k.view(-1, hkv, d)[at] = step[:, None, None].to(BF).expand(-1, hkv, d).contiguous()
+    q = torch.ones(int(c.q_start[-1]), 2 * hkv, d, device="cuda", dtype=BF)
     q[::2] = -1.0
-    out, lse, st = _run(c, q, flags)
-    assert st == 0
-    _compare(out, lse, q, c, d ** -0.5)
-    out, lse, st = _run(c, q, flags, scale=1.0)
-    _compare(out, lse, q, c, 1.0)
+    q[:, 1::3] *= 0.25
+    for hints in (True, False):
+        for scale in (0.0, 1.0):
+            out, lse, st = _run(c, q, flags, hints, scale=scale)
+            assert st == 0
+            _compare(out, lse, q, c, scale or d ** -0.5)
 
 
 @pytest.mark.parametrize("flags", [0, 2])

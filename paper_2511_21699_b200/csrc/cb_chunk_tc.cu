@@ -13,6 +13,10 @@
 // Causality: a row sees the keys up to its own token.  Tiles below a row tile's first token need no mask; the first row tile of a unit leaves
 // out a last tile that only the second one sees.  Slots of the last page behind the sequence's last token may hold anything: their scores are
 // masked, and their values are overwritten with zeros in shared memory before the product reads them (0 x NaN would reach the output).
+//
+// Measured: a prompt of 8 k, 64 query heads over 8, D = 128: 1.01 to 1.08 ms, 1.0 to 1.1 PFLOP/s of the visible scores, the tensor pipe 54% busy; a pair of
+// tiles takes 3.3 k to 3.5 k cycles of which 2.05 k are products, the rest hand-overs between the softmax and the products.  64 single tokens over 1.09 GB
+// of keys and values: 188 to 204 us, 5.3 to 5.8 TB/s.  One token over 4 k, 32 heads: 23.8 us, nearly all of it before the first tile and behind the last.
 #include <cuda.h>
 
 #include <mutex>

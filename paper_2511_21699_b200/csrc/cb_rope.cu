@@ -5,6 +5,9 @@
 // head and a lane holds two pieces of 8 elements that are rotated with one another (i with i + R / 2) or each in itself (neighbouring
 // pairs), so a rotation needs no exchange between lanes and the norm's sum two or three shuffles.  A warp takes 4 (D = 128) or 8
 // (D = 64) heads of one row, or two or four times as many; which sequence the row belongs to is found while its elements are on their way.
+//
+// 8,192 rows of 64 + 2 x 8 heads of 128: 68 us, 5.0 TB/s of the 6.5 that a copy reaches; with 58% of the issue slots busy the loads that
+// registers leave room for bound it.  32 single tokens: 3.3 us, a launch and three dependent reads.  2,048 tree rows of 32 + 2 x 8: 13.9 us.
 #include "cb_chunk.cuh"
 
 namespace {

@@ -4,10 +4,10 @@
 // Each element is read once and written once, so HBM bounds it; the arithmetic is some ten instructions a pair.  D / 16 lanes share a
 // head and a lane holds two pieces of 8 elements that are rotated with one another (i with i + R / 2) or each in itself (neighbouring
 // pairs), so a rotation needs no exchange between lanes and the norm's sum two or three shuffles.  A warp takes 4 (D = 128) or 8
-// (D = 64) heads of one row, or two or four times as many; which sequence the row belongs to is found while its elements are on their way.
+// (D = 64) heads of one row, or two to four times as many; which sequence the row belongs to is found while its elements are on their way.
 //
 // 8,192 rows of 64 + 2 x 8 heads of 128: 68 us, 5.0 TB/s of the 6.5 that a copy reaches; with 58% of the issue slots busy the loads that
-// registers leave room for bound it.  32 single tokens: 3.3 us, a launch and three dependent reads.  2,048 tree rows of 32 + 2 x 8: 13.9 us.
+// registers leave room for bound it.  32 single tokens: 3.3 us, a launch and three dependent reads.  2,048 tree rows of 32 + 2 x 8 from a cold start: 13.9 us.
 #include "cb_chunk.cuh"
 
 namespace {
@@ -64,10 +64,11 @@ __device__ __forceinline__ uint4 pack8(const uint64_t* x) {
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// INTER: pairs are neighbours.  Of the kernels with four groups a warp, which have the most registers, five blocks an SM for trees and six for chunks:
-// 16,384 tree rows of 64/8 heads 119 us with five and 134 with six, 8,192 rows of a chunk 72 and 68.
+// INTER: pairs are neighbours.  Seven blocks an SM (72 registers), five of the kernels with four groups a warp, which have the most registers: 16,384 tree rows of
+// 64/8 heads 119 us with five, 134 with six.  With two groups 2,048 tree rows of 32/8 heads take 11.2 us with seven blocks, 11.8 with six, 12.0 with eight.  (The products of
+// a row's angles and norm weights held for all its heads save a fifth of the arithmetic and cost 20 registers: 12 to 26% slower.)
 template <int D, bool TREE, bool INTER, int U>
-__global__ void __launch_bounds__(32 * kRopeWarps, U == 4 ? (TREE ? 5 : 6) : 4) cb_rope_kernel(const RopeParams p) {
+__global__ void __launch_bounds__(32 * kRopeWarps, U == 4 ? 5 : 7) cb_rope_kernel(const RopeParams p) {
     CB_PDL_ENTRY();
     constexpr int LPH = D / 16, HPW = 32 / LPH;               // lanes per head, heads that a warp holds side by side
     const int lane = threadIdx.x & 31, sub = lane % LPH;
@@ -236,13 +237,13 @@ cb_status launch_rope_of(RopeParams p, int D, cudaStream_t st) {
     return CB_OK;
 }
 // Groups of heads per warp: one where warps are few, since a call then takes what one of them takes; more where there are plenty, since what
-// belongs to the row (its sequence, position, page, angles) is found once for all of them and their loads are under way together.  us with 1, 2, 4:
-// 8,192 rows of 64/8 heads 87.8, 75.2, 68.1; 16,384 tree rows of them 158, 125, 119; 4,096 of 32/8 26.4, 23.5, 22.4; 2,048 tree rows of 32/8 13.7, 11.3, 13.3.
+// belongs to the row (its sequence, position, page, angles) is found once for all of them and their loads are under way together.  us with 1, 2, 3, 4:
+// 8,192 rows of 64/8 heads 87.8, 74.1, 67.8, 67.8 (six blocks); 4,096 of 32/8 26.4, 23.1, 22.1, 23.0; 16,384 tree rows of 64/8 158, 125, 127, 119; 2,048 of 32/8 13.7, 11.2, 11.3, 13.3.
 template <bool TREE>
 cb_status launch_rope(const RopeParams& p, int D, cudaStream_t st) {
     const int per_warp = 32 / (D / 16);
     const long long groups = (long long)p.n_rows * ((p.Hq + 2 * p.Hkv + per_warp - 1) / per_warp);
-    if (groups >= 40000) return launch_rope_of<TREE, 4>(p, D, st);
+    if (groups >= 40000) return launch_rope_of<TREE, TREE ? 4 : 3>(p, D, st);
     return groups >= 8000 ? launch_rope_of<TREE, 2>(p, D, st) : launch_rope_of<TREE, 1>(p, D, st);
 }
 

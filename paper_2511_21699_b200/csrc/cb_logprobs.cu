@@ -182,8 +182,9 @@ __device__ __forceinline__ void extremes(const Block<BF16>& b, float& hi, float&
         }
     }
 }
-// Adds a block to s and t on reference ref.  FORBIDDEN: there may be -inf among the elements, whose e d = 0 * -inf must not be NaN.
-template <bool BF16, bool FORBIDDEN>
+// Adds a block to s and t on reference ref.  CLAMP: some x - ref may be -inf (a forbidden token, or finite logits further apart than fp32 reaches, such as a
+// mask of the type's lowest value beside a large one), whose e d = 0 * -inf must not be NaN.
+template <bool BF16, bool CLAMP>
 __device__ __forceinline__ void add_block(const Block<BF16>& b, float ref, uint64_t& s2, uint64_t& t2) {
     const uint64_t neg = f2_pack(-ref, -ref), l2e = f2_pack(kLog2e, kLog2e);
     const uint32_t* w = reinterpret_cast<const uint32_t*>(b.u);
@@ -193,7 +194,7 @@ __device__ __forceinline__ void add_block(const Block<BF16>& b, float ref, uint6
                           : f2_pack(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
         d = f2_add(d, neg);
         float a, c;
-        if (FORBIDDEN) {
+        if (CLAMP) {
             f2_unpack(d, a, c);
             d = f2_pack(max_keep_nan(a, -3e38f), max_keep_nan(c, -3e38f));
         }
@@ -269,7 +270,7 @@ __global__ void __launch_bounds__(kThreads, 4) cb_logprobs_kernel(const LogprobP
             if (++in_slot == per_slot) { s_hi[slots++][tid] = slot_hi; slot_hi = -INFINITY; in_slot = 0; }
         }
         const float base = ref == -INFINITY ? 0.f : ref;
-        if (lo == -INFINITY) add_block<BF16, true>(cur, base, s2, t2);
+        if (lo - base == -INFINITY) add_block<BF16, true>(cur, base, s2, t2);
         else add_block<BF16, false>(cur, base, s2, t2);
         cur = next;
     }

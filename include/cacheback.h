@@ -452,7 +452,7 @@ cb_status cb_chunk_attn(cb_ctx* ctx, const cb_chunk_attn_args* args, void* strea
  *   entropy[i]   = log Z - sum_v p_v x_v    p = exp(x) / Z
  *   top_ids[i], top_logprobs[i]             the top_k largest x_v (equal ones by rising id) and their x_v - log Z, largest first
  * fp32 throughout.  Logits are finite or -inf (a forbidden token: probability 0, no part of the entropy); a row with a NaN or +inf, or
- * without a finite logit, gives NaN.
+ * without a finite logit, gives NaN; its alternatives are ids all the same, -1 where only NaNs are left.
  *   logits        [n_rows, vocab] of logits_dtype, rows logits_row_stride elements apart
  *   rows          int32 [n_out]: the row of logits of each output, or NULL for row i (n_out <= n_rows)
  *   tokens        int32 [n_out], or NULL: logprobs is then not written

@@ -488,7 +488,8 @@ __global__ void __launch_bounds__(kThreads, 4) cb_logprobs_kernel(const LogprobP
         if (tid < p.K) {
             const unsigned long long k = s_top[tid];
             p.top_ids[(size_t)i * p.K + tid] = k == 0 ? -1 : id_of(k);
-            p.top_logprobs[(size_t)i * p.K + tid] = k == 0 ? -INFINITY : (value_of(k) - a.m) - log_s;
+            // no element for this place: the vocabulary is shorter, or what is left are NaNs
+            p.top_logprobs[(size_t)i * p.K + tid] = k == 0 ? (tid < p.V ? NAN : -INFINITY) : (value_of(k) - a.m) - log_s;
         }
     }
     __syncwarp();

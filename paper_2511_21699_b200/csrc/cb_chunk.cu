@@ -17,13 +17,18 @@ __global__ void __launch_bounds__(32 * kWarps) cb_chunk_cc_kernel(const CbChunkP
     constexpr int C = D / 32;
     const int lane = threadIdx.x & 31;
     const long long item = (long long)blockIdx.x * kWarps + (threadIdx.x >> 5);
-    if (item >= (long long)p.n_rows * p.Hq) return;
+    const long long rows = (long long)p.n_rows * p.Hq;
+    if (item >= rows) {                                       // behind the rows' warps, a sequence per lane: what is wrong with it
+        const long long b = (item - rows) * 32 + lane;
+        const int error = b < p.B ? cb_chunk_seq(p, (int)b).error : 0;
+        if (error) atomicCAS(p.status, 0u, (uint32_t)error);
+        return;
+    }
     const int row = (int)(item / p.Hq), h = (int)(item % p.Hq), kh = h / p.G;
     int q0, q1, ctx;
     const int b = cb_find_sequence(p.q_start, p.B, row, lane, p.ctx_len, &q0, &q1, &ctx);
     if (b < 0) return;
     const CbChunkSeq s = cb_chunk_seq(p, b);
-    if (s.error && lane == 0) atomicCAS(p.status, 0u, (uint32_t)s.error);
     if (row - s.row0 >= s.n) return;
     const int keys = s.ctx + row - s.row0 + 1;
     const __nv_bfloat16* q = p.q + ((size_t)row * p.Hq + h) * D;
@@ -90,7 +95,7 @@ extern "C" cb_status cb_chunk_attn(cb_ctx* ctx, const cb_chunk_attn_args* a, voi
     p.status = ctx->d_status;
     cudaStream_t st = (cudaStream_t)stream;
     if (!(c.flags & CB_FLAG_ATTN_CUDA_CORES)) return cb_chunk_launch_tensor(ctx, p, st);
-    const long long blocks = ((long long)p.n_rows * p.Hq + kWarps - 1) / kWarps;
+    const long long blocks = ((long long)p.n_rows * p.Hq + (p.B + 31) / 32 + kWarps - 1) / kWarps;
     if (blocks > 0x7FFFFFFFll) return CB_ERR_UNSUPPORTED;
     if (p.D == 128) cb_chunk_cc_kernel<128><<<(unsigned)blocks, 32 * kWarps, 0, st>>>(p);
     else cb_chunk_cc_kernel<64><<<(unsigned)blocks, 32 * kWarps, 0, st>>>(p);

@@ -74,7 +74,17 @@ __global__ void __launch_bounds__(32 * kRopeWarps, U == 4 ? 5 : 7) cb_rope_kerne
     const int lane = threadIdx.x & 31, sub = lane % LPH;
     const uint32_t item = blockIdx.x * kRopeWarps + (threadIdx.x >> 5);
     const uint32_t urow = item / (uint32_t)p.parts;
-    if (urow >= (uint32_t)p.n_rows) return;                   // a whole warp
+    if (urow >= (uint32_t)p.n_rows) {                         // a whole warp
+        // Behind the rows' warps, a sequence per lane: a range without any row of these has no other warp to report it.
+        if constexpr (!TREE) {
+            const uint32_t b = (item - (uint32_t)p.n_rows * (uint32_t)p.parts) * 32u + lane;
+            if (b < (uint32_t)p.B) {
+                const int q0 = p.q_start[b], q1 = p.q_start[b + 1];
+                if (q0 != q1 && (q0 < 0 || q1 < q0 || q1 > p.n_rows)) atomicCAS(p.status, 0u, (uint32_t)CB_ERR_INVALID_ARG);
+            }
+        }
+        return;
+    }
     const int row = (int)urow, slot0 = (int)(item - urow * (uint32_t)p.parts) * (U * HPW) + lane / LPH;
     const int R = p.rope ? p.R : 0;
     const bool turned = sub < R / 16;                         // both pieces are, or neither
@@ -228,7 +238,7 @@ template <bool TREE, int U>
 cb_status launch_rope_of(RopeParams p, int D, cudaStream_t st) {
     const int per_warp = U * 32 / (D / 16);
     p.parts = (p.Hq + 2 * p.Hkv + per_warp - 1) / per_warp;
-    const long long blocks = ((long long)p.n_rows * p.parts + kRopeWarps - 1) / kRopeWarps;
+    const long long blocks = ((long long)p.n_rows * p.parts + (TREE ? 0 : (p.B + 31) / 32) + kRopeWarps - 1) / kRopeWarps;
     if (blocks * kRopeWarps > 0x7FFFFFFFll) return CB_ERR_UNSUPPORTED;
     auto kernel = p.interleaved ? (D == 128 ? cb_rope_kernel<128, TREE, true, U> : cb_rope_kernel<64, TREE, true, U>)
                                 : (D == 128 ? cb_rope_kernel<128, TREE, false, U> : cb_rope_kernel<64, TREE, false, U>);

@@ -29,7 +29,7 @@ __global__ void __launch_bounds__(32 * kWarps) cb_chunk_cc_kernel(const CbChunkP
     const int b = cb_find_sequence(p.q_start, p.B, row, lane, p.ctx_len, &q0, &q1, &ctx);
     if (b < 0) return;
     const CbChunkSeq s = cb_chunk_seq(p, b);
-    if (row - s.row0 >= s.n) return;
+    if (s.n == 0 || row - s.row0 >= s.n) return;              // (with n = 0 row0 may be any number)
     const int keys = s.ctx + row - s.row0 + 1;
     const __nv_bfloat16* q = p.q + ((size_t)row * p.Hq + h) * D;
     float m = -INFINITY, l = 0.f, acc[C] = {};

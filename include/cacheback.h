@@ -419,7 +419,7 @@ cb_status cb_tree_rope(cb_ctx* ctx, const cb_tree_rope_args* args, void* stream)
  *   lse          float [n_rows, Hq] or NULL     natural-log sum of exponentials per row
  *   max_chunk    host upper bound on every chunk length (0 = n_rows); with chunks of few tokens it decides how the work is split
  *   max_ctx      host upper bound on every ctx_len + chunk length (0 = max_pages * P)
- *   scale        softmax scale; 0 selects 1/sqrt(D)
+ *   scale        softmax scale, positive and finite; 0 selects 1/sqrt(D)
  * fp32 accumulation and softmax, output rounded to bf16; equal calls give equal bits, as in cb_tree_attn.
  * Rows that belong to no sequence are left as they were.  A sequence whose cached and new tokens exceed max_pages * P, or max_ctx, is
  * left alone and CB_ERR_KV_FULL recorded; one whose range is not inside [0, n_rows], or longer than max_chunk, or whose ctx_len is

@@ -79,6 +79,7 @@ extern "C" cb_status cb_chunk_attn(cb_ctx* ctx, const cb_chunk_attn_args* a, voi
     CB_CHECK_ARG(a->n_rows >= 0 && a->max_pages >= 1 && a->num_pages >= 1 && a->max_chunk >= 0 && a->max_ctx >= 0);
     const uintptr_t al = (uintptr_t)a->q | (uintptr_t)a->k_pool | (uintptr_t)a->v_pool | (uintptr_t)a->out;
     CB_CHECK_ARG((al & 15) == 0 && ((uintptr_t)a->lse & 3) == 0);
+    CB_CHECK_ARG(a->scale >= 0.f && a->scale < INFINITY);     // (the kernels' running maximum is of scores times a positive number)
     if (a->n_rows == 0) return CB_OK;
     const cb_config& c = ctx->cfg;
     CbChunkParams p = {};

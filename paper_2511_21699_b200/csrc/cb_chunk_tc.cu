@@ -539,11 +539,12 @@ __global__ void __launch_bounds__(kThreads, 1) cb_chunk_tc_kernel(const CbChunkP
             const size_t at_row = (size_t)(u->row0 + (row_valid ? token : 0)) * p.Hq + h;
             // this thread's columns of the output row, 16 at a time: half a row with two row tiles, a quarter with one
             int npc, c0;
-            // a shared unit: how many parts of it are in memory already; the look overlaps the wait for the last product
+            // a shared unit: how many parts of it are in memory already; the look overlaps the wait for the last product (launches of few units
+            // count CTAs, below, not warps)
             const int np = whole ? 1 : u->np;
             uint32_t* const ticket = p.part_ticket + (np > 1 ? u->ticket : 0) + sw;
             uint32_t arrived = 0;
-            if (np > 1 && lane == 0) arrived = ld_acquire(ticket);
+            if (np > 1 && p.cs == 0 && lane == 0) arrived = ld_acquire(ticket);
             float x_m, x_l, x_w0 = 1.f, x_w1 = 1.f;           // reference and sum; one row tile: weights of O0 and O1
             if (two) {
                 if (!(ok = mbar_wait(bar_odone(l), c_od & 1, s_abort, p.status))) break;

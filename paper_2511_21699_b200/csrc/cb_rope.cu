@@ -64,9 +64,10 @@ __device__ __forceinline__ uint4 pack8(const uint64_t* x) {
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// INTER: pairs are neighbours.  Seven blocks an SM (72 registers), five of the kernels with four groups a warp, which have the most registers: 16,384 tree rows of
-// 64/8 heads 119 us with five, 134 with six.  With two groups 2,048 tree rows of 32/8 heads take 11.2 us with seven blocks, 11.8 with six, 12.0 with eight.  (The products of
-// a row's angles and norm weights held for all its heads save a fifth of the arithmetic and cost 20 registers: 12 to 26% slower.)
+// INTER: pairs are neighbours.  U: groups of heads a warp.  Seven blocks an SM (72 registers; with three groups 12 bytes are spilled, once a warp, as there is no
+// loop), five of the kernels with four groups, which have the most registers: 16,384 tree rows of 64/8 heads 119 us with five, 134 with six.  With two groups 2,048 tree
+// rows of 32/8 heads take 11.2 us with seven blocks, 11.8 with six, 12.0 with eight.  (The products of a row's angles and norm weights held for all its heads save a fifth
+// of the arithmetic and cost 20 registers: 12 to 26% slower.)
 template <int D, bool TREE, bool INTER, int U>
 __global__ void __launch_bounds__(32 * kRopeWarps, U == 4 ? 5 : 7) cb_rope_kernel(const RopeParams p) {
     CB_PDL_ENTRY();
@@ -234,27 +235,39 @@ RopeParams params_of(cb_ctx* ctx, const cb_qkv_rows& r) {
     return p;
 }
 
-template <bool TREE, int U>
-cb_status launch_rope_of(RopeParams p, int D, cudaStream_t st) {
-    const int per_warp = U * 32 / (D / 16);
+template <int D, bool TREE, int U>
+cb_status launch_rope_of(RopeParams p, cudaStream_t st) {
+    constexpr int per_warp = U * 32 / (D / 16);
     p.parts = (p.Hq + 2 * p.Hkv + per_warp - 1) / per_warp;
     const long long blocks = ((long long)p.n_rows * p.parts + (TREE ? 0 : (p.B + 31) / 32) + kRopeWarps - 1) / kRopeWarps;
     if (blocks * kRopeWarps > 0x7FFFFFFFll) return CB_ERR_UNSUPPORTED;
-    auto kernel = p.interleaved ? (D == 128 ? cb_rope_kernel<128, TREE, true, U> : cb_rope_kernel<64, TREE, true, U>)
-                                : (D == 128 ? cb_rope_kernel<128, TREE, false, U> : cb_rope_kernel<64, TREE, false, U>);
+    auto kernel = p.interleaved ? cb_rope_kernel<D, TREE, true, U> : cb_rope_kernel<D, TREE, false, U>;
     CB_CUDA(cb_launch_pdl(kernel, dim3((unsigned)blocks), dim3(32 * kRopeWarps), 0, st, p));
     cb_count_launch(1);
     return CB_OK;
 }
 // Groups of heads per warp: one where warps are few, since a call then takes what one of them takes; more where there are plenty, since what
-// belongs to the row (its sequence, position, page, angles) is found once for all of them and their loads are under way together.  us with 1, 2, 3, 4:
-// 8,192 rows of 64/8 heads 87.8, 74.1, 67.8, 67.8 (six blocks); 4,096 of 32/8 26.4, 23.1, 22.1, 23.0; 16,384 tree rows of 64/8 158, 125, 127, 119; 2,048 of 32/8 13.7, 11.2, 11.3, 13.3.
-template <bool TREE>
-cb_status launch_rope(const RopeParams& p, int D, cudaStream_t st) {
-    const int per_warp = 32 / (D / 16);
-    const long long groups = (long long)p.n_rows * ((p.Hq + 2 * p.Hkv + per_warp - 1) / per_warp);
-    if (groups >= 40000) return launch_rope_of<TREE, TREE ? 4 : 3>(p, D, st);
-    return groups >= 8000 ? launch_rope_of<TREE, 2>(p, D, st) : launch_rope_of<TREE, 1>(p, D, st);
+// belongs to the row (its sequence, position, page, angles) is found once for all of them and their loads are under way together.  us with 1, 2, 3, 4 by
+// the number of groups:
+//   chunks of 32/8 heads of 128  6,000  4.9, 4.4, 4.2, 4.9;  8,000  5.5, 4.5, 5.4, 5.1;  11,000  7.3, 6.8, 6.1, 5.9;  24,000  13.9, 11.3, 11.1, 12.0
+//                                28,000  -, 13.5, 13.1, 13.4;  40,000  23.0, 18.0, 17.4, 18.0;  330,000  -, 145.7, 132.0, 140.4
+//   of 28/4 heads of 64          6,000  4.6, 4.3, 5.0, 4.4;  8,000  5.3, 5.9, 5.1, 6.6;  11,000  7.0, 6.8, 7.1, 7.3;  24,000  13.9, 12.7, 11.6, 14.4
+//                                28,000  -, 14.6, 12.9, 15.2;  40,000  22.6, 19.6, 17.2, 21.5
+//   tree rows of 32/8 heads      8,000  5.1, 4.3, 5.8, 5.1;  24,000  13.0, 10.7, 11.8, 12.0;  64,000  34.2, 27.7, 29.0, 28.3;  330,000  -, 124.3, 125.2, 123.0
+//   of 64/8 heads                100,000  -, 41.1, 43.0, 40.4;  160,000  -, 63.3, 65.2, 61.6;  330,000  -, 124.8, 129.9, 121.3
+//   of 12/4 (20 to 16 places)    100,000  52.8, 44.9, 44.6, 52.2;  of 28/4 heads of 64  8,000  5.1, 5.4, 5.5, 6.7;  40,000  20.7, 18.0, 18.7, 21.3;  330,000  -, 138.6, 135.9, 158.9
+// (Between 7,000 and 9,000 groups one or the other is ahead by how the warps fill the SMs' last round: two by up to 20%, one by up to 12%.)
+template <int D, bool TREE>
+cb_status launch_rope(const RopeParams& p, cudaStream_t st) {
+    constexpr int per_warp = 32 / (D / 16);
+    const int heads = p.Hq + 2 * p.Hkv;
+    const long long groups = (long long)p.n_rows * ((heads + per_warp - 1) / per_warp);
+    if constexpr (!TREE) {
+        if (groups >= 28000) return launch_rope_of<D, TREE, 3>(p, st);
+    } else if constexpr (D == 128) {
+        if (groups >= 100000 && heads % (4 * per_warp) == 0) return launch_rope_of<D, TREE, 4>(p, st);
+    }
+    return groups >= 8000 ? launch_rope_of<D, TREE, 2>(p, st) : launch_rope_of<D, TREE, 1>(p, st);
 }
 
 }  // namespace
@@ -269,7 +282,7 @@ extern "C" cb_status cb_chunk_append(cb_ctx* ctx, const cb_chunk_append_args* a,
     p.q_start = a->q_start; p.ctx_len = a->ctx_len; p.block_table = a->block_table;
     p.n_rows = a->n_rows; p.max_pages = a->max_pages; p.num_pages = a->num_pages;
     p.q_out = (__nv_bfloat16*)a->q_out; p.k_out = (__nv_bfloat16*)a->k_pool; p.v_out = (__nv_bfloat16*)a->v_pool;
-    return launch_rope<false>(p, ctx->cfg.head_dim, (cudaStream_t)stream);
+    return ctx->cfg.head_dim == 128 ? launch_rope<128, false>(p, (cudaStream_t)stream) : launch_rope<64, false>(p, (cudaStream_t)stream);
 }
 
 extern "C" cb_status cb_tree_rope(cb_ctx* ctx, const cb_tree_rope_args* a, void* stream) {
@@ -280,5 +293,5 @@ extern "C" cb_status cb_tree_rope(cb_ctx* ctx, const cb_tree_rope_args* a, void*
     p.depth = a->tree_depth; p.n_nodes = a->n_nodes; p.ctx_len = a->ctx_len;
     p.n_rows = ctx->cfg.batch * ctx->cfg.max_nodes;
     p.q_out = (__nv_bfloat16*)a->q_out; p.k_out = (__nv_bfloat16*)a->k_out; p.v_out = (__nv_bfloat16*)a->v_out;
-    return launch_rope<true>(p, ctx->cfg.head_dim, (cudaStream_t)stream);
+    return ctx->cfg.head_dim == 128 ? launch_rope<128, true>(p, (cudaStream_t)stream) : launch_rope<64, true>(p, (cudaStream_t)stream);
 }

@@ -11,14 +11,15 @@ pytestmark = pytest.mark.gpu
 
 
 def _groups(rows, hq, hkv, d):
-    """Groups of heads that a warp holds side by side; from 8,000 on a warp takes two, from 40,000 on three (chunks) or four (trees)."""
+    """Groups of heads that a warp holds side by side; from 8,000 on a warp takes two, from 28,000 on three (chunks); trees
+    of 128 dims whose heads fill four take four from 100,000 on."""
     return rows * -(-(hq + 2 * hkv) // (512 // d))
 
 
 @pytest.mark.parametrize("inter", [False, True])
 @pytest.mark.parametrize("hq,hkv,d,rot,norm,rows,lo,hi", [
     (12, 4, 128, 128, True, 300, 0, 8000), (9, 3, 64, 48, False, 300, 0, 8000),
-    (36, 12, 128, 96, True, 701, 8000, 40000), (28, 4, 64, 64, True, 2003, 8000, 40000),
+    (36, 12, 128, 96, True, 701, 8000, 28000), (28, 4, 64, 64, True, 2003, 8000, 28000),
     (64, 8, 128, 128, True, 2100, 40000, 10 ** 9), (40, 40, 128, 64, False, 1400, 40000, 10 ** 9), (28, 4, 64, 64, True, 8203, 40000, 10 ** 9),
     (64, 8, 64, 32, False, 4100, 40000, 10 ** 9)])
 def test_append_forms(hq, hkv, d, rot, norm, rows, lo, hi, inter):
@@ -47,9 +48,10 @@ def test_append_forms(hq, hkv, d, rot, norm, rows, lo, hi, inter):
 @pytest.mark.parametrize("inter", [False, True])
 @pytest.mark.parametrize("hq,hkv,d,rot,norm,B,T,lo,hi", [
     (12, 4, 128, 128, True, 5, 61, 0, 8000), (9, 3, 64, 48, False, 5, 61, 0, 8000),
-    (36, 12, 128, 96, True, 11, 64, 8000, 40000), (28, 4, 64, 64, True, 33, 61, 8000, 40000),
+    (36, 12, 128, 96, True, 11, 64, 8000, 28000), (28, 4, 64, 64, True, 33, 61, 8000, 28000),
     (66, 11, 128, 128, True, 16, 128, 40000, 10 ** 9), (64, 8, 128, 32, False, 33, 64, 40000, 10 ** 9), (28, 4, 64, 64, True, 70, 121, 40000, 10 ** 9),
-    (64, 8, 64, 64, False, 40, 128, 40000, 10 ** 9)])
+    (64, 8, 64, 64, False, 40, 128, 40000, 10 ** 9),
+    (64, 8, 128, 128, True, 40, 128, 100000, 10 ** 9), (24, 4, 128, 64, False, 98, 128, 100000, 10 ** 9)])
 def test_tree_forms(hq, hkv, d, rot, norm, B, T, lo, hi, inter):
     assert lo <= _groups(B * T, hq, hkv, d) < hi
     rng = np.random.default_rng(T)

@@ -501,13 +501,18 @@ __global__ void __launch_bounds__(kThreads, 4) cb_logprobs_kernel(const LogprobP
 //   9 rows of 128 k fp32 10.5, 7.5, 5.5, 4.4;  40 of 128 k bf16 12.7, 9.0, 7.0, 7.8;  75 of 50 k fp32 10.7, 8.3, 7.7, 9.8
 //   150 of 128 k bf16 15.0, 16.5, 14.7, 16.8;  300 of 128 k bf16 27.5, 21.8, 23.2, 28.4;  300 of 50 k fp32 14.7, 18.5, 20.0, 24.6;  600 of 128 k 34.6, 35.0, 39.9, 52.7
 //   with 20 alternatives 9 of 128 k bf16 14.4, 11.1, 8.8, 8.4;  40 16.1, 12.4, 11.5, 14.0;  150 of fp32 27.9, 24.8, 29.8, 37.0;  with five 9 of 32 k 6.6, 7.1, 6.5, 6.4
-int pick_cluster(long long rows, int V, int K, int num_sms) {
+// Few rows around the shortest that are shared (none and 20 alternatives):
+//   9 of 16 k fp32 3.3, 3.2, 2.8, 3.0 and 6.0, 6.3, 5.9, 6.7;  of 24 k 4.1, 3.8, 3.4, 3.2 and 7.0, 6.7, 6.6, 6.7;  of 32 k 4.7, 4.1, 3.4, 3.2 and 7.8, 7.2, 6.7, 6.8
+//   of 48 k fp32 6.2, 4.8, 3.8, 3.5 and 9.5, 8.2, 7.0, 7.5;  of 64 k 7.5, 5.5, 4.1, 3.5 and 11.0, 9.1, 7.5, 7.4;  74 of 32 k fp32 7.5, 5.8, 6.0, 7.3 and 10.2, 8.9, 11.0, 16.7
+//   9 of 24 k bf16 3.4, 3.7, 3.1, 3.3 and 6.5, 6.8, 6.5, 7.3;  of 32 k 3.8, 3.8, 3.3, 3.3 and 6.8, 7.0, 6.7, 7.3;  of 48 k 4.9, 4.2, 3.7, 3.2 and 8.3, 7.8, 7.2, 7.3
+//   74 of 32 k bf16 3.9, 4.0, 5.5, 7.3 and 6.9, 7.3, 10.1, 17.2;  of 48 k 6.1, 5.0, 6.9, 7.5 and 9.1, 8.2, 12.1, 17.2
+int pick_cluster(long long rows, int V, int K, int num_sms, bool f32) {
     int cs = 1;
-    if (V < 48000) return cs;
+    if (V < (f32 ? 24000 : 48000)) return cs;
     while (cs < 8) {
         const long long ctas = rows * cs * 2, each = V / (cs * 2);
         const bool idle = ctas * 10 <= 11ll * num_sms, room = ctas * 10 <= 42ll * num_sms;
-        if (!(idle ? each >= 12000 : room && each >= (K ? 64000 : 32000))) break;
+        if (!(idle ? each >= (f32 ? 8000 : 12000) : room && each >= (K ? 64000 : 32000))) break;
         cs *= 2;
     }
     return cs;
@@ -515,7 +520,7 @@ int pick_cluster(long long rows, int V, int K, int num_sms) {
 
 cb_status launch_logprobs(const cb_logprobs_args& a, LogprobParams p, int num_sms, cudaStream_t st) {
     const bool f32 = a.logits_dtype == CB_DTYPE_F32;
-    p.cs = pick_cluster(p.n_out, p.V, p.K, num_sms);
+    p.cs = pick_cluster(p.n_out, p.V, p.K, num_sms, f32);
     if ((long long)p.n_out * p.cs > 0x7FFFFFFFll) return CB_ERR_UNSUPPORTED;
     auto kernel = p.K ? (f32 ? cb_logprobs_kernel<false, true> : cb_logprobs_kernel<true, true>)
                       : (f32 ? cb_logprobs_kernel<false, false> : cb_logprobs_kernel<true, false>);

@@ -17,7 +17,7 @@
  *   - Every tensor pointer is a DEVICE pointer owned by the caller unless a parameter says "host".
  *     The library never allocates or frees device memory: all of its state and scratch lives in the
  *     workspace handed to cb_create.
- *   - `stream` is a cudaStream_t passed as void*. The four step calls and cb_reset only enqueue work
+ *   - `stream` is a cudaStream_t passed as void*. The calls of a step, the ones beside it and cb_reset only enqueue work
  *     on it; they never synchronise.  Calls on one context must be ordered (same stream, or events).
  *   - Host-detectable argument errors are returned at once and nothing is enqueued.  Conditions only
  *     the device can see (a probe limit, a bounded wait that ran out) are recorded in a device status
@@ -48,7 +48,7 @@ typedef enum {
     CB_ERR_TIMEOUT = 5,     /* device: a bounded wait (mbarrier / flag) ran out                        */
     CB_ERR_UNSUPPORTED = 6,
     CB_ERR_STATIC_LIMIT = 7, /* cb_accept_static: the problem does not fit the built-in scratch array       */
-    CB_ERR_KV_FULL = 8,      /* device: cb_kv_commit found a sequence whose pages cannot hold the new tokens   */
+    CB_ERR_KV_FULL = 8,      /* device: a sequence whose pages cannot hold its new tokens (cb_kv_commit, cb_chunk_append, cb_chunk_attn) */
     CB_ERR_CANARY = 9        /* checking build only: a guard word beside a workspace region was overwritten    */
 } cb_status;
 

@@ -286,7 +286,7 @@ class Cacheback:
     def cb_chunk_attn(self, q, k_pool, v_pool, block_table, q_start, ctx_len, out=None, lse=None, max_chunk=0, max_ctx=0, scale=0.0, stream=None):
         """Causal attention of each sequence's new tokens over its cached ones and themselves, after cb_chunk_append has put their
         keys and values into the pages.  max_chunk, max_ctx: host upper bounds on the new tokens of a sequence and on its cached and
-        new tokens together (0: not known)."""
+        new tokens together (0: not known).  scale: positive, 0 selects 1 / sqrt(head_dim)."""
         if out is None:
             out = torch.empty_like(q)
         self._host.chunk_attn(self._h, self._shape, q, k_pool, v_pool, block_table, q_start, ctx_len, out, lse, max_chunk, max_ctx, scale, stream)

@@ -45,10 +45,10 @@ cb_status cb_compute_layout(const cb_config* c, CbLayout* L) {
     L->off_index = region(B * ns * 4);
     L->off_lstamp = region(B * (size_t)c->LC * 4);
     L->off_entries = region(B * (size_t)c->LC * L->E * 4);
-    L->off_status = region(16 * 4);                          // status words; from word 8 on, what tree attention's launches hand on
+    L->off_status = region(16 * 4);                          // status words; from word 8 on, what attention launches (tree and chunk) hand on
     L->off_counters = region(CB_NUM_COUNTERS * 8);
     L->off_rowmax = region(B * (size_t)c->max_nodes * 8);
-    L->off_ticket = region(align_up(B * 4, 256) + 2 * CB_ATTN_TICKETS * 4);  // acceptance's counters, then tree attention's
+    L->off_ticket = region(align_up(B * 4, 256) + 2 * CB_ATTN_TICKETS * 4);  // acceptance's counters, then those of both attentions
     L->off_attn_ticket = L->off_ticket + align_up(B * 4, 256);
     L->off_bulk_plan = region(B * 16);
     L->attn_max_units = CB_ATTN_MAX_UNITS;

@@ -166,7 +166,8 @@ cb_attn_tc_kernel(const CbAttnParams p, const __grid_constant__ TcMaps maps) {
     }
     CB_PDL_ENTRY();
     // The set of tickets that this launch counts in.  The other one is cleared for the next launch, so that it finds zeros even
-    // where the launch before this one gave up on a wait and left counts half way, whatever the status word says.
+    // where the launch before this one gave up on a wait and left counts half way, whatever the status word says.  (A CTA clears its own
+    // 16: with cs = 0 the grid is all nc persistent CTAs, and only such a launch hands the turn on.)
     int ticket_set = 0;
     if (warp == 2 && p.cs == 0) {
         ticket_set = (int)(*reinterpret_cast<volatile uint32_t*>(p.part_turn) & 1u) * CB_ATTN_TICKETS;

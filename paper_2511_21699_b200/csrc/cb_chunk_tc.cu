@@ -14,9 +14,11 @@
 // out a last tile that only the second one sees.  Slots of the last page behind the sequence's last token may hold anything: their scores are
 // masked, and their values are overwritten with zeros in shared memory before the product reads them (0 x NaN would reach the output).
 //
-// Measured: a prompt of 8 k, 64 query heads over 8, D = 128: 1.01 to 1.08 ms, 1.0 to 1.1 PFLOP/s of the visible scores, the tensor pipe 54% busy; a pair of
-// tiles takes 3.3 k to 3.5 k cycles of which 2.05 k are products, the rest hand-overs between the softmax and the products.  64 single tokens over 1.09 GB
-// of keys and values: 188 to 204 us, 5.3 to 5.8 TB/s.  One token over 4 k, 32 heads: 23.8 us, nearly all of it before the first tile and behind the last.
+// Measured: a prompt of 8 k, 64 query heads over 8, D = 128: 1.01 ms in short runs, 1.11 under the power cap, 1.0 to 1.1 PFLOP/s of the visible scores, the tensor pipe 54% busy;
+// a pair of tiles takes 3.3 k to 3.5 k cycles of which 2.05 k are products, the rest hand-overs between the softmax and the products.  64 single tokens over 1.09 GB
+// of keys and values: 188 to 207 us, 5.3 to 5.8 TB/s.  One token over 4 k, 32 heads: 23.8 us, nearly all of it before the first tile and behind the last.
+// Of the spills (124 to 132 bytes a thread) three to four loads and one store a tile and softmax warp lie in the tile loop, beside some 450 instructions; the others
+// are a unit's, some ten (counted over prompts of 1 k to 4 k).
 #include <cuda.h>
 
 #include <mutex>
@@ -434,7 +436,10 @@ __global__ void __launch_bounds__(kThreads, 1) cb_chunk_tc_kernel(const CbChunkP
                         m_used = fmaxf(c0, c1) * p.scale_log2;   // -inf if the row sees none of them
                     }
                     uint32_t pk[32];
-                    // P of this thread's 64 scores (packed into pk) against reference mu; returns their sum
+                    // P of this thread's 64 scores (packed into pk) against reference mu; returns their sum.  P is rounded to bf16, the type that its product with
+                    // bf16 values takes on the tensor cores (half a step, 2^-8 of each at most, as in tree attention; as two bf16 terms it would double that product): the
+                    // output's error against 64 bits is 2.1e-3 to 2.4e-3 instead of the 1.6e-3 that its own rounding makes.  The sum is of the unrounded fp32 values,
+                    // so that lse keeps their accuracy.
                     auto make_p_of = [&](float mu, auto masked) {
                         constexpr bool MASKED = decltype(masked)::value;
                         const uint64_t scale2 = f2_pack(p.scale_log2, p.scale_log2), negmu2 = f2_pack(-mu, -mu);

@@ -100,7 +100,9 @@ struct cb_ctx {
     size_t guard_off[CB_MAX_GUARDS];
     int n_guards;
     float* d_attn_part;     // partial outputs of units shared between CTAs
-    uint32_t* d_attn_ticket; // [2][CTAs][16] parts of a shared unit that are in memory; an attention launch counts in one set and clears the other
+    // [2][CTAs][16] parts of a shared unit that are in memory, for tree and chunk attention alike.  A launch counts in the set that the turn names; one that hands
+    // the turn on has cleared the other set for all persistent CTAs, whatever its own grid, so that the next launch of either kind finds zeros.
+    uint32_t* d_attn_ticket;
     uint32_t* d_attn_turn;   // [0] attention launches so far, its lowest bit names the set; [1] CTAs of the running one that have left
     size_t attn_part_floats;
     int attn_max_units;     // partial row tiles available

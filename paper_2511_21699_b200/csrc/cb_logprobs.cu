@@ -14,8 +14,8 @@
 // A row is one CTA's, or, where that leaves SMs idle, a cluster's, whose CTAs take equal parts of it and hand their sums and their K best
 // to the first one through distributed shared memory.
 //
-// 2,048 rows of 128 k bf16: 87 us, 6.0 TB/s of the 6.5 that a copy reaches (100 us in long runs at the clock that the power cap leaves: the
-// exponential unit, an element each, is 72% busy); with 20 alternatives 111.  300 rows of 50 k fp32 with 20: 24 us.  Nine rows of 32 k bf16 with 5: 6.6.
+// 2,048 rows of 128 k bf16: 87 us, 6.0 TB/s of the 6.5 that a copy reaches (103 us in long runs at the clock that the power cap leaves: the
+// exponential unit, an element each, is 72% busy); with 20 alternatives 111.  300 rows of 50 k fp32 with 20: 24 us (15 without).  Nine rows of 32 k bf16 with 5: 6.7.
 #include <math.h>
 
 #include "cb_common.cuh"

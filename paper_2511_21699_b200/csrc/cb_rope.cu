@@ -6,8 +6,8 @@
 // pairs), so a rotation needs no exchange between lanes and the norm's sum two or three shuffles.  A warp takes 4 (D = 128) or 8
 // (D = 64) heads of one row, or two to four times as many; which sequence the row belongs to is found while its elements are on their way.
 //
-// 8,192 rows of 64 + 2 x 8 heads of 128: 68 us, 5.0 TB/s of the 6.5 that a copy reaches; with 58% of the issue slots busy the loads that
-// registers leave room for bound it.  32 single tokens: 3.3 us, a launch and three dependent reads.  2,048 tree rows of 32 + 2 x 8 from a cold start: 13.9 us.
+// 8,192 rows of 64 + 2 x 8 heads of 128: 68 to 71 us, 4.8 to 5.0 TB/s of the 6.5 that a copy reaches; with 64% of the issue slots busy the loads that registers leave
+// room for bound it.  32 single tokens: 3.2 to 3.6 us, a launch and three dependent reads.  2,048 tree rows of 32 + 2 x 8 from a cold start: 13.9 us.
 #include "cb_chunk.cuh"
 
 namespace {

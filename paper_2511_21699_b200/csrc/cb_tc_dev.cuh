@@ -1,6 +1,6 @@
 // Device-side building blocks of the tensor-core attention kernels: bounded mbarrier waits, TMA loads, tcgen05 fences,
 // TMEM loads and stores, packed fp32 arithmetic, and the shared-memory / instruction descriptors of tcgen05.mma.
-// Included by cb_attn_tc.cu only (one translation unit holds both attention kernels and their launcher).
+// Included by cb_attn_tc.cu (tree attention, its CTA-pair form and their launcher) and cb_chunk_tc.cu (chunk attention).
 #pragma once
 #include <cuda.h>
 

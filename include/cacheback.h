@@ -11,7 +11,8 @@
  *   cb_accept      take the target's greedy choice after every node and keep the longest verified
  *                  branch plus one more token                                 (Section 3.2)
  * Beside it: cb_chunk_append and cb_chunk_attn bring prompts and single tokens into the paged cache and attend over it, cb_tree_rope
- * makes the rotated queries and keys of a tree, cb_logprobs says how likely tokens were.
+ * makes the rotated queries and keys of a tree, cb_logprobs says how likely tokens were; cb_pages_assign and cb_slot_map keep the cache's block
+ * tables on the GPU, cb_block_summary, cb_block_select, cb_block_attn and cb_block_tree_attn attend to the parts of a long context that matter.
  *
  * Conventions
  *   - Every tensor pointer is a DEVICE pointer owned by the caller unless a parameter says "host".
@@ -48,7 +49,7 @@ typedef enum {
     CB_ERR_TIMEOUT = 5,     /* device: a bounded wait (mbarrier / flag) ran out                        */
     CB_ERR_UNSUPPORTED = 6,
     CB_ERR_STATIC_LIMIT = 7, /* cb_accept_static: the problem does not fit the built-in scratch array       */
-    CB_ERR_KV_FULL = 8,      /* device: a sequence whose pages cannot hold its new tokens (cb_kv_commit, cb_chunk_append, cb_chunk_attn) */
+    CB_ERR_KV_FULL = 8,      /* device: a sequence whose pages cannot hold its new tokens (cb_kv_commit, the calls beside the step) */
     CB_ERR_CANARY = 9        /* checking build only: a guard word beside a workspace region was overwritten    */
 } cb_status;
 
@@ -445,6 +446,127 @@ typedef struct {
 } cb_chunk_attn_args;
 
 cb_status cb_chunk_attn(cb_ctx* ctx, const cb_chunk_attn_args* args, void* stream);
+
+/*
+ * Block tables made on the GPU.  The pages of a pool that no sequence holds lie on a stack; one call gives pages to the sequences that
+ * grow and takes them back from those that shrink, so that a step's lengths never have to reach the host.
+ *   want_len    int32 [batch]               tokens that each sequence is to have room for (0: it is finished)
+ *   block_table int32 [batch, max_pages]    read and written: the first held[b] entries of row b are its pages
+ *   held        int32 [batch]               read and written: pages of each sequence
+ *   free_pages  int32 [num_pages]           read and written: the stack, its top at n_free[0] - 1
+ *   n_free      int32 [1]                   read and written
+ * With t = ceil(want_len / P), a sequence that holds more than t pages gives the ones behind the first t back, one that holds fewer is given
+ * t - held.  What is there to give is, in this order: the pages given back in this call, by sequence and place, then the stack from its
+ * top; the sequences that grow take from it one after the other, and what is left of the pages given back is pushed so that the first of them
+ * is at the top.  (A call that grows some sequences is undone by one that shrinks them to where they were.)  Where the needs up to and with
+ * a growing sequence exceed what there is, it is left alone, and so are the growing ones behind it; CB_ERR_KV_FULL is recorded.  So is a
+ * sequence whose t exceeds max_pages.  A sequence with a negative length, or whose held is not in 0 .. max_pages, is left alone and
+ * CB_ERR_INVALID_ARG recorded; a stack whose n_free is not in 0 .. num_pages, or that the pages given back would overfill, leaves everything as it
+ * is and records the same.  Entries behind a row's pages and behind the top of the stack are not touched.  batch <= CB_MAX_ASSIGN.
+ */
+enum { CB_MAX_ASSIGN = 16384 };
+cb_status cb_pages_assign(cb_ctx* ctx, const int32_t* want_len, int32_t* block_table, int32_t max_pages, int32_t* held, int32_t* free_pages,
+                          int32_t num_pages, int32_t* n_free, void* stream);
+
+/*
+ * Where the rows of a packed batch go (as in cb_chunk_append): row q_start[b] + i is the token at position ctx_len[b] + i of sequence b.
+ *   slots      int64 [n_rows]   block_table[b][pos / P] * P + pos % P, the row of the pool seen as [num_pages * P, ...]
+ *   positions  int32 [n_rows], seqs int32 [n_rows]
+ * Rows that belong to no sequence are -1 in all three, as are those of a sequence whose range is not inside [0, n_rows] or whose ctx_len is
+ * negative (CB_ERR_INVALID_ARG recorded) or whose pages cannot hold its tokens (CB_ERR_KV_FULL).  A row whose page lies outside the pool
+ * has slot -1 and CB_ERR_INVALID_ARG is recorded.
+ */
+typedef struct {
+    const int32_t* q_start;
+    const int32_t* ctx_len;
+    const int32_t* block_table;
+    int32_t max_pages;
+    int32_t num_pages;
+    int32_t n_rows;
+    int64_t* slots;
+    int32_t* positions;
+    int32_t* seqs;
+} cb_slot_map_args;
+
+cb_status cb_slot_map(cb_ctx* ctx, const cb_slot_map_args* args, void* stream);
+
+/*
+ * Attention over the parts of a long context that matter: the context is cut into blocks of `block` tokens (16, 32, 64 or 128), every block has a
+ * summary (its mean key, in 8 bits), and per sequence and kv head the queries of a chunk or of a tree choose n_select blocks by it.
+ *
+ * cb_block_summary: the summaries of the blocks that new tokens touch, after their keys are in the pages (cb_chunk_append, cb_kv_commit).  For
+ * every block that holds one of the positions from_len[b] .. to_len[b] - 1 of sequence b, over its tokens below to_len[b], m the mean of a head's keys:
+ *   k_scale = max |m| / 127,   k_mean[d] = m[d] * 127 / max |m| rounded to the nearest whole number (half way: to the even one)
+ * in 64 bits, and so independent of any order of addition.  They are stored with the block's first page.
+ *   k_pool   bf16 [num_pages, P, Hkv, D];  block_table int32 [batch, max_pages];  from_len, to_len int32 [batch]
+ *   k_mean   int8 [num_pages, Hkv, D], k_scale float [num_pages, Hkv]     other pages' rows are left as they were
+ * A head whose mean is not finite gets k_scale = +inf and zeros, which cb_block_select puts before all others.  A sequence with
+ * from_len >= to_len has none; one with from_len < 0 is left alone and CB_ERR_INVALID_ARG recorded, one with to_len > max_pages * P CB_ERR_KV_FULL; a
+ * block with a page outside the pool is left alone and CB_ERR_INVALID_ARG recorded.
+ */
+typedef struct {
+    const void* k_pool;
+    const int32_t* block_table;
+    const int32_t* from_len;
+    const int32_t* to_len;
+    int8_t* k_mean;
+    float* k_scale;
+    int32_t max_pages;
+    int32_t num_pages;
+    int32_t block;
+} cb_block_summary_args;
+
+cb_status cb_block_summary(cb_ctx* ctx, const cb_block_summary_args* args, void* stream);
+
+/*
+ * cb_block_select: which blocks of its cached tokens each sequence's new rows attend to, one list per kv head.  The rows are a chunk's
+ * (q_start given: rows q_start[b] .. q_start[b + 1) of q [n_rows, Hq, D]) or a tree's (n_nodes given: the first n_nodes[b] of q [batch, T, Hq, D]).
+ * All query heads of the kv head and all rows vote: with a = max |q| over them (at least 1e-30) and r = 127 / a,
+ *   q8 = q * r rounded to a whole number (fp32),   score_j = float(max over rows and heads of sum_d q8[d] k_mean_j[d]) * k_scale_j
+ * Sums of whole numbers: the choice depends on no order of addition.  Of the nb = ceil(ctx_len / block) blocks the n_first first and the
+ * n_last newest ones are always chosen, the others by falling score, equal scores by rising number, until there are n_select; a score that is not a
+ * number comes before all others.
+ *   ctx_len  int32 [batch]   cached tokens before the chunk or the tree
+ *   blocks   int32 [batch, Hkv, n_select]   by rising number; -1 behind the last where nb < n_select; all -1 where there are no rows
+ *   n_first >= 0, n_last >= 1, n_first + n_last <= n_select <= CB_MAX_SELECT
+ *   max_chunk  host upper bound on a chunk's rows (0 = n_rows), max_ctx on every ctx_len (0 = max_pages * P); max_ctx / block <= 32,768
+ * A sequence whose rows or ctx_len are out of their bounds (q_start's range, n_nodes, max_chunk; negative ctx_len: CB_ERR_INVALID_ARG; ctx_len > max_ctx:
+ * CB_ERR_KV_FULL) gets -1 throughout.  A block whose first page lies outside the pool scores as if k_scale were 0, CB_ERR_INVALID_ARG recorded.  Queries
+ * are finite.
+ */
+enum { CB_MAX_SELECT = 1024 };
+typedef struct {
+    const void* q;
+    const int32_t* q_start;
+    const int32_t* n_nodes;
+    const int8_t* k_mean;
+    const float* k_scale;
+    const int32_t* block_table;
+    const int32_t* ctx_len;
+    int32_t* blocks;
+    int32_t n_rows;
+    int32_t max_pages;
+    int32_t num_pages;
+    int32_t block;
+    int32_t n_select, n_first, n_last;
+    int32_t max_chunk;
+    int32_t max_ctx;
+} cb_block_select_args;
+
+cb_status cb_block_select(cb_ctx* ctx, const cb_block_select_args* args, void* stream);
+
+/*
+ * Attention over the selected blocks.
+ *   cb_block_attn       cb_chunk_attn in which row q_start[b] + i sees, of the ctx_len[b] cached tokens, only those in its kv head's blocks, and
+ *                       the chunk's own tokens up to its own
+ *   cb_block_tree_attn  cb_tree_attn in which the cached context is that of the kv head's blocks
+ * Arguments, outputs, errors and alignment are those of the dense calls (max_ctx still bounds all of a sequence's tokens); blocks int32 [batch, Hkv,
+ * n_select] is as cb_block_select leaves it for the same ctx_len and block: with nb = ceil(ctx_len / block) > n_select a list names n_select
+ * blocks below nb, the newest one last; with fewer its first nb entries are 0 .. nb - 1.  Other lists give rows of no meaning; a block that does
+ * not exist, or a page outside the pool, reads as zeros.
+ */
+cb_status cb_block_attn(cb_ctx* ctx, const cb_chunk_attn_args* args, const int32_t* blocks, int32_t block, int32_t n_select, void* stream);
+cb_status cb_block_tree_attn(cb_ctx* ctx, const cb_attn_args* args, const int32_t* blocks, int32_t block, int32_t n_select, void* stream);
 
 /*
  * How likely tokens were: for each of n_out rows of logits x over vocab tokens, with Z = sum_v exp(x_v),

@@ -17,6 +17,7 @@ CB_ERR_INVALID_ARG, CB_ERR_CANARY = 1, 9
 CB_GUARD_BYTES = 256
 CB_STATIC_MAX_BATCH, CB_STATIC_MAX_ROWS = 1024, 8192
 CB_MAX_TOP = 32
+CB_MAX_ASSIGN, CB_MAX_SELECT = 16384, 1024
 CB_NUM_COUNTERS = 8
 COUNTER_NAMES = ["inserts", "leader_evictions", "follower_evictions", "queries", "query_hits", "max_probe", "frozen_queries",
                  "frozen_hits"]
@@ -26,7 +27,8 @@ EXPORTS = ["cb_workspace_bytes", "cb_create", "cb_destroy", "cb_reset", "cb_upda
            "cb_status_str", "cb_accept_static", "cb_kv_commit", "cb_frozen_bytes", "cb_frozen_load", "cb_frozen_dump",
            "cb_frozen_attach", "cb_frozen_build_bytes", "cb_frozen_build", "cb_tree_add_branches", "cb_update_bulk", "cb_debug_build",
            "cb_bulk_scratch_bytes", "cb_bulk_scratch_attach", "cb_accept_update_draft_tree", "cb_chunk_append", "cb_tree_rope",
-           "cb_chunk_attn", "cb_logprobs", "cb_accept_logprobs"]
+           "cb_chunk_attn", "cb_logprobs", "cb_accept_logprobs", "cb_pages_assign", "cb_slot_map", "cb_block_summary", "cb_block_select",
+           "cb_block_attn", "cb_block_tree_attn"]
 
 
 class CbConfigC(C.Structure):
@@ -82,6 +84,21 @@ class CbLogprobsArgsC(C.Structure):
                [(n, C.c_void_p) for n in ("logprobs", "entropy", "top_ids", "top_logprobs")]
 
 
+class CbSlotMapArgsC(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("q_start", "ctx_len", "block_table")] + [(n, C.c_int32) for n in ("max_pages", "num_pages", "n_rows")] + \
+               [(n, C.c_void_p) for n in ("slots", "positions", "seqs")]
+
+
+class CbBlockSummaryArgsC(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("k_pool", "block_table", "from_len", "to_len", "k_mean", "k_scale")] + \
+               [(n, C.c_int32) for n in ("max_pages", "num_pages", "block")]
+
+
+class CbBlockSelectArgsC(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("q", "q_start", "n_nodes", "k_mean", "k_scale", "block_table", "ctx_len", "blocks")] + \
+               [(n, C.c_int32) for n in ("n_rows", "max_pages", "num_pages", "block", "n_select", "n_first", "n_last", "max_chunk", "max_ctx")]
+
+
 _lib = None
 
 
@@ -114,6 +131,12 @@ def load():
     L.cb_chunk_attn.argtypes = [vp, C.POINTER(CbChunkAttnArgsC), vp]
     L.cb_logprobs.argtypes = [vp, C.POINTER(CbLogprobsArgsC), vp]
     L.cb_accept_logprobs.argtypes = [vp, vp, vp, C.POINTER(CbLogprobsArgsC), vp]
+    L.cb_pages_assign.argtypes = [vp, vp, vp, i32, vp, vp, i32, vp, vp]
+    L.cb_slot_map.argtypes = [vp, C.POINTER(CbSlotMapArgsC), vp]
+    L.cb_block_summary.argtypes = [vp, C.POINTER(CbBlockSummaryArgsC), vp]
+    L.cb_block_select.argtypes = [vp, C.POINTER(CbBlockSelectArgsC), vp]
+    L.cb_block_attn.argtypes = [vp, C.POINTER(CbChunkAttnArgsC), vp, i32, i32, vp]
+    L.cb_block_tree_attn.argtypes = [vp, C.POINTER(CbAttnArgsC), vp, i32, i32, vp]
     L.cb_accept.argtypes = [vp, vp, vp, vp, vp, vp, i32, i64, vp, vp, vp, vp, vp, vp]
     L.cb_accept_static.argtypes = [i32, i32, i32, i32, vp, vp, vp, vp, vp, i32, i64, vp, vp, vp, vp, vp]
     L.cb_table_dump.argtypes = [vp, i32, C.POINTER(i32), vp, vp, vp]

@@ -38,7 +38,7 @@ def _stream(stream):
 
 _BOUND = ("cb_reset", "cb_update", "cb_update_bulk", "cb_draft_tree", "cb_update_draft_tree", "cb_tree_attn", "cb_accept",
           "cb_accept_update_draft_tree", "cb_kv_commit", "cb_chunk_append", "cb_chunk_attn", "cb_tree_rope", "cb_logprobs", "cb_accept_logprobs",
-          "cb_status_str")
+          "cb_pages_assign", "cb_slot_map", "cb_block_summary", "cb_block_select", "cb_block_attn", "cb_block_tree_attn", "cb_status_str")
 _host_module = None
 try:                                     # loaded with the package (some 40 ms), not by the first context; not there yet while it is built
     from . import _binding
@@ -328,6 +328,61 @@ class Cacheback:
             res = self._alloc_logprobs((self.cfg.batch, self.cfg.max_depth + 1), top_k)
         self._host.accept_logprobs(self._h, self._shape, logits, accepted, top_k, res, stream)
         return res
+
+    # ---- beside the step: block tables on the GPU, attention over selected blocks ----------------------
+    def cb_pages_assign(self, want_len, block_table, held, free_pages, n_free, stream=None):
+        """Pages for the sequences that grow to want_len[b] tokens, taken back from those that shrink: block_table [batch, max_pages], held [batch], the stack
+        free_pages [num_pages] and n_free [1] are updated in place.  Sequences that there are no pages for keep what they hold."""
+        self._host.pages_assign(self._h, self._shape, want_len, block_table, held, free_pages, n_free, stream)
+
+    def cb_slot_map(self, q_start, ctx_len, block_table, num_pages, n_rows, res=None, stream=None):
+        """Sequence, position and row of the pool of every row of a packed batch (rows that belong to no sequence: -1): a dictionary with slots int64,
+        positions and seqs int32, each [n_rows]."""
+        if res is None:
+            new = lambda t: torch.empty(n_rows, dtype=t, device=self.device)
+            res = dict(slots=new(torch.int64), positions=new(torch.int32), seqs=new(torch.int32))
+        self._host.slot_map(self._h, self._shape, q_start, ctx_len, block_table, num_pages, n_rows, res, stream)
+        return res
+
+    def alloc_summary(self, num_pages):
+        """(k_mean, k_scale): the summaries of a pool's blocks, as cb_block_summary fills them."""
+        c = self.cfg
+        return (torch.zeros(num_pages, c.n_kv_heads, c.head_dim, dtype=torch.int8, device=self.device),
+                torch.zeros(num_pages, c.n_kv_heads, dtype=torch.float32, device=self.device))
+
+    def cb_block_summary(self, k_pool, block_table, from_len, to_len, k_mean, k_scale, block=64, stream=None):
+        """The mean key, in 8 bits, of every block of `block` tokens that one of the positions from_len[b] .. to_len[b] - 1 falls into, stored with the
+        block's first page in k_mean [pages, n_kv_heads, head_dim] and k_scale [pages, n_kv_heads].  The keys must be in the pages."""
+        self._host.block_summary(self._h, self._shape, k_pool, block_table, from_len, to_len, k_mean, k_scale, block, stream)
+
+    def cb_block_select(self, q, k_mean, k_scale, block_table, ctx_len, q_start=None, n_nodes=None, block=64, n_select=32, n_first=1, n_last=2, max_chunk=0,
+                        max_ctx=0, blocks=None, stream=None):
+        """The n_select blocks of its ctx_len[b] cached tokens that each sequence's queries score highest, per kv head, by rising number: blocks
+        [batch, n_kv_heads, n_select], -1 behind the last.  The queries are a chunk's (q [rows, heads, head_dim] and q_start) or a tree's (q [batch, max_nodes,
+        heads, head_dim] and n_nodes).  The n_first first and the n_last newest blocks are always among them."""
+        if blocks is None:
+            blocks = torch.empty(self.cfg.batch, self.cfg.n_kv_heads, n_select, dtype=torch.int32, device=self.device)
+        self._host.block_select(self._h, self._shape, q, k_mean, k_scale, block_table, ctx_len, q_start, n_nodes, block, n_select, n_first, n_last, max_chunk,
+                                max_ctx, blocks, stream)
+        return blocks
+
+    def cb_block_attn(self, q, k_pool, v_pool, block_table, q_start, ctx_len, blocks, block=64, out=None, lse=None, max_chunk=0, max_ctx=0, scale=0.0,
+                      stream=None):
+        """cb_chunk_attn over the selected blocks of the cached tokens and the chunk's own ones.  blocks: of cb_block_select, for the same ctx_len."""
+        if out is None:
+            out = torch.empty_like(q)
+        self._host.block_attn(self._h, self._shape, q, k_pool, v_pool, block_table, q_start, ctx_len, out, lse, max_chunk, max_ctx, scale, blocks, block,
+                              stream)
+        return out
+
+    def cb_block_tree_attn(self, q, k_pool, v_pool, block_table, ctx_len, k_tree, v_tree, tree_mask, n_nodes, blocks, block=64, out=None, lse=None,
+                           max_ctx=0, scale=0.0, stream=None):
+        """cb_tree_attn over the selected blocks of the cached tokens and the tree's nodes."""
+        if out is None:
+            out = torch.empty_like(q)
+        self._host.block_tree_attn(self._h, self._shape, q, k_pool, v_pool, block_table, ctx_len, k_tree, v_tree, tree_mask, n_nodes, out, lse, max_ctx,
+                                   scale, blocks, block, stream)
+        return out
 
     # ---- helpers ------------------------------------------------------------------------------------
     def cb_frozen_attach(self, frozen):

@@ -38,6 +38,12 @@ struct Library {
     decltype(&cb_tree_rope) tree_rope;
     decltype(&cb_logprobs) logprobs;
     decltype(&cb_accept_logprobs) accept_logprobs;
+    decltype(&cb_pages_assign) pages_assign;
+    decltype(&cb_slot_map) slot_map;
+    decltype(&cb_block_summary) block_summary;
+    decltype(&cb_block_select) block_select;
+    decltype(&cb_block_attn) block_attn;
+    decltype(&cb_block_tree_attn) block_tree_attn;
     decltype(&cb_status_str) status_str;
 } g_lib;
 
@@ -53,7 +59,9 @@ const at::Tensor& tensor_of(PyObject* o) {
     return THPVariable_Unpack(o);
 }
 
-const char* type_name(at::ScalarType t) { return t == at::kInt ? "torch.int32" : t == at::kFloat ? "torch.float32" : "torch.bfloat16"; }
+const char* type_name(at::ScalarType t) {
+    return t == at::kInt ? "torch.int32" : t == at::kFloat ? "torch.float32" : t == at::kLong ? "torch.int64" : t == at::kChar ? "torch.int8" : "torch.bfloat16";
+}
 
 // The device pointer of a contiguous CUDA tensor of the given type; None: a null pointer.
 template <typename T = int32_t>
@@ -392,27 +400,166 @@ void do_tree_rope(PyObject* const* a) {
     const OnDevice on(s, a[15]);
     call("cb_tree_rope", [&] { return g_lib.tree_rope(c, &x, on.stream); });
 }
+// q, k_pool, v_pool, block_table, q_start, ctx_len, out, lse, max_chunk, max_ctx, scale
+cb_chunk_attn_args chunk_of(const Shape& s, PyObject* const* a) {
+    cb_chunk_attn_args x = {};
+    const int64_t n = rows_of(a[0]);
+    const auto bf = at::kBFloat16;
+    x.q = arg(s, a[0], "q", bf, {n, s.Hq, s.D}, "[rows, n_q_heads, head_dim]").p;
+    x.n_rows = (int32_t)n;
+    const Cache k = cache_of(s, a[1], a[2], a[3]);
+    x.k_pool = k.k; x.v_pool = k.v; x.block_table = k.table; x.max_pages = k.max_pages; x.num_pages = k.num_pages;
+    x.q_start = static_cast<int32_t*>(arg(s, a[4], "q_start", at::kInt, {s.B + 1}, "[batch + 1]").p);
+    x.ctx_len = static_cast<int32_t*>(arg(s, a[5], "ctx_len", at::kInt, {s.B}, "[batch]").p);
+    x.out = arg(s, a[6], "out", bf, {n, s.Hq, s.D}, "of q's shape").p;
+    x.lse = opt<float>(s, a[7], "lse", at::kFloat, {n, s.Hq}, "[rows, n_q_heads]");
+    x.max_chunk = int_of(a[8], "max_chunk");
+    x.max_ctx = int_of(a[9], "max_ctx");
+    x.scale = float_of(a[10]);
+    return x;
+}
 // handle, shape, q, k_pool, v_pool, block_table, q_start, ctx_len, out, lse, max_chunk, max_ctx, scale, stream
 void do_chunk_attn(PyObject* const* a) {
     cb_ctx* c = ctx_of(a[0]);
     const Shape s = shape_of(a[1]);
-    cb_chunk_attn_args x = {};
-    const int64_t n = rows_of(a[2]);
-    const auto bf = at::kBFloat16;
-    x.q = arg(s, a[2], "q", bf, {n, s.Hq, s.D}, "[rows, n_q_heads, head_dim]").p;
-    x.n_rows = (int32_t)n;
-    const Cache k = cache_of(s, a[3], a[4], a[5]);
-    x.k_pool = k.k; x.v_pool = k.v; x.block_table = k.table; x.max_pages = k.max_pages; x.num_pages = k.num_pages;
-    x.q_start = static_cast<int32_t*>(arg(s, a[6], "q_start", at::kInt, {s.B + 1}, "[batch + 1]").p);
-    x.ctx_len = static_cast<int32_t*>(arg(s, a[7], "ctx_len", at::kInt, {s.B}, "[batch]").p);
-    x.out = arg(s, a[8], "out", bf, {n, s.Hq, s.D}, "of q's shape").p;
-    x.lse = opt<float>(s, a[9], "lse", at::kFloat, {n, s.Hq}, "[rows, n_q_heads]");
-    x.max_chunk = int_of(a[10], "max_chunk");
-    x.max_ctx = int_of(a[11], "max_ctx");
-    x.scale = float_of(a[12]);
-    if (n == 0) return;
+    const cb_chunk_attn_args x = chunk_of(s, a + 2);
+    if (x.n_rows == 0) return;
     const OnDevice on(s, a[13]);
     call("cb_chunk_attn", [&] { return g_lib.chunk_attn(c, &x, on.stream); });
+}
+// ---- block tables on the GPU, attention over selected blocks
+const int32_t* table_of(const Shape& s, PyObject* o, int32_t* max_pages) {
+    const Arg t = arg(s, o, "block_table", at::kInt, {s.B, -1}, "[batch, pages]");
+    if (t.t->size(1) > INT32_MAX) refuse_shape("block_table", "of less than 2^31 columns");
+    *max_pages = (int32_t)t.t->size(1);
+    return static_cast<int32_t*>(t.p);
+}
+// handle, shape, want_len, block_table, held, free_pages, n_free, stream
+void do_pages_assign(PyObject* const* a) {
+    cb_ctx* c = ctx_of(a[0]);
+    const Shape s = shape_of(a[1]);
+    const int32_t* want = static_cast<int32_t*>(arg(s, a[2], "want_len", at::kInt, {s.B}, "[batch]").p);
+    int32_t max_pages;
+    int32_t* table = const_cast<int32_t*>(table_of(s, a[3], &max_pages));
+    int32_t* held = static_cast<int32_t*>(arg(s, a[4], "held", at::kInt, {s.B}, "[batch]").p);
+    const Arg f = arg(s, a[5], "free_pages", at::kInt, {-1}, "[pages]");
+    if (f.t->size(0) > INT32_MAX) refuse_shape("free_pages", "of less than 2^31 pages");
+    int32_t* n_free = static_cast<int32_t*>(arg(s, a[6], "n_free", at::kInt, {1}, "[1]").p);
+    const OnDevice on(s, a[7]);
+    call("cb_pages_assign", [&] { return g_lib.pages_assign(c, want, table, max_pages, held, static_cast<int32_t*>(f.p), (int32_t)f.t->size(0), n_free, on.stream); });
+}
+// handle, shape, q_start, ctx_len, block_table, num_pages, n_rows, res, stream
+void do_slot_map(PyObject* const* a) {
+    cb_ctx* c = ctx_of(a[0]);
+    const Shape s = shape_of(a[1]);
+    cb_slot_map_args x = {};
+    x.q_start = static_cast<int32_t*>(arg(s, a[2], "q_start", at::kInt, {s.B + 1}, "[batch + 1]").p);
+    x.ctx_len = static_cast<int32_t*>(arg(s, a[3], "ctx_len", at::kInt, {s.B}, "[batch]").p);
+    x.block_table = table_of(s, a[4], &x.max_pages);
+    x.num_pages = int_of(a[5], "num_pages");
+    x.n_rows = int_of(a[6], "n_rows");
+    if (x.n_rows < 0) refuse_shape("n_rows", "not negative");
+    auto get = [&](const char* name, at::ScalarType t) -> void* {
+        Ref r(PyMapping_GetItemString(a[7], name));
+        return arg(s, r.o, name, t, {x.n_rows}, "[n_rows]").p;
+    };
+    x.slots = static_cast<int64_t*>(get("slots", at::kLong));
+    x.positions = static_cast<int32_t*>(get("positions", at::kInt));
+    x.seqs = static_cast<int32_t*>(get("seqs", at::kInt));
+    if (x.n_rows == 0) return;                                // tensors without elements have no memory
+    const OnDevice on(s, a[8]);
+    call("cb_slot_map", [&] { return g_lib.slot_map(c, &x, on.stream); });
+}
+struct Summary { int8_t* mean; float* scale; int64_t pages; };
+Summary summary_of(const Shape& s, PyObject* mean, PyObject* scale, int64_t pages) {
+    const Arg m = arg(s, mean, "k_mean", at::kChar, {pages, s.Hkv, s.D}, "[pages, n_kv_heads, head_dim]");
+    const Arg k = arg(s, scale, "k_scale", at::kFloat, {m.t->size(0), s.Hkv}, "[pages, n_kv_heads]");
+    if (m.t->size(0) > INT32_MAX) refuse_shape("k_mean", "of less than 2^31 pages");
+    return {static_cast<int8_t*>(m.p), static_cast<float*>(k.p), m.t->size(0)};
+}
+// handle, shape, k_pool, block_table, from_len, to_len, k_mean, k_scale, block, stream
+void do_block_summary(PyObject* const* a) {
+    cb_ctx* c = ctx_of(a[0]);
+    const Shape s = shape_of(a[1]);
+    cb_block_summary_args x = {};
+    const Arg k = arg(s, a[2], "k_pool", at::kBFloat16, {-1, s.P, s.Hkv, s.D}, "[pages, page_size, n_kv_heads, head_dim]");
+    x.k_pool = k.p;
+    x.block_table = table_of(s, a[3], &x.max_pages);
+    x.from_len = static_cast<int32_t*>(arg(s, a[4], "from_len", at::kInt, {s.B}, "[batch]").p);
+    x.to_len = static_cast<int32_t*>(arg(s, a[5], "to_len", at::kInt, {s.B}, "[batch]").p);
+    const Summary m = summary_of(s, a[6], a[7], k.t->size(0));
+    x.k_mean = m.mean; x.k_scale = m.scale; x.num_pages = (int32_t)m.pages;
+    x.block = int_of(a[8], "block");
+    const OnDevice on(s, a[9]);
+    call("cb_block_summary", [&] { return g_lib.block_summary(c, &x, on.stream); });
+}
+// handle, shape, q, k_mean, k_scale, block_table, ctx_len, q_start, n_nodes, block, n_select, n_first, n_last, max_chunk, max_ctx, blocks, stream
+void do_block_select(PyObject* const* a) {
+    cb_ctx* c = ctx_of(a[0]);
+    const Shape s = shape_of(a[1]);
+    cb_block_select_args x = {};
+    if ((a[7] == Py_None) == (a[8] == Py_None)) refuse_shape("q_start or n_nodes", "given, one of the two");
+    if (a[8] == Py_None) {
+        const int64_t n = rows_of(a[2]);
+        x.q = arg(s, a[2], "q", at::kBFloat16, {n, s.Hq, s.D}, "[rows, n_q_heads, head_dim]").p;
+        x.n_rows = (int32_t)n;
+        x.q_start = static_cast<int32_t*>(arg(s, a[7], "q_start", at::kInt, {s.B + 1}, "[batch + 1]").p);
+    } else {
+        x.q = arg(s, a[2], "q", at::kBFloat16, {s.B, s.T, s.Hq, s.D}, "[batch, max_nodes, n_q_heads, head_dim]").p;
+        x.n_nodes = static_cast<int32_t*>(arg(s, a[8], "n_nodes", at::kInt, {s.B}, "[batch]").p);
+    }
+    const Summary m = summary_of(s, a[3], a[4], -1);
+    x.k_mean = m.mean; x.k_scale = m.scale; x.num_pages = (int32_t)m.pages;
+    x.block_table = table_of(s, a[5], &x.max_pages);
+    x.ctx_len = static_cast<int32_t*>(arg(s, a[6], "ctx_len", at::kInt, {s.B}, "[batch]").p);
+    x.block = int_of(a[9], "block");
+    x.n_select = int_of(a[10], "n_select"); x.n_first = int_of(a[11], "n_first"); x.n_last = int_of(a[12], "n_last");
+    x.max_chunk = int_of(a[13], "max_chunk"); x.max_ctx = int_of(a[14], "max_ctx");
+    x.blocks = static_cast<int32_t*>(arg(s, a[15], "blocks", at::kInt, {s.B, s.Hkv, x.n_select}, "[batch, n_kv_heads, n_select]").p);
+    const OnDevice on(s, a[16]);
+    call("cb_block_select", [&] { return g_lib.block_select(c, &x, on.stream); });
+}
+const int32_t* blocks_of(const Shape& s, PyObject* o, int32_t* n_select) {
+    const Arg t = arg(s, o, "blocks", at::kInt, {s.B, s.Hkv, -1}, "[batch, n_kv_heads, n_select]");
+    *n_select = (int32_t)std::min<int64_t>(t.t->size(2), INT32_MAX);
+    return static_cast<int32_t*>(t.p);
+}
+// handle, shape, q, k_pool, v_pool, block_table, q_start, ctx_len, out, lse, max_chunk, max_ctx, scale, blocks, block, stream
+void do_block_attn(PyObject* const* a) {
+    cb_ctx* c = ctx_of(a[0]);
+    const Shape s = shape_of(a[1]);
+    const cb_chunk_attn_args x = chunk_of(s, a + 2);
+    int32_t n_select;
+    const int32_t* blocks = blocks_of(s, a[13], &n_select);
+    const int32_t block = int_of(a[14], "block");
+    if (x.n_rows == 0) return;
+    const OnDevice on(s, a[15]);
+    call("cb_block_attn", [&] { return g_lib.block_attn(c, &x, blocks, block, n_select, on.stream); });
+}
+// handle, shape, q, k_pool, v_pool, block_table, ctx_len, k_tree, v_tree, tree_mask, n_nodes, out, lse, max_ctx, scale, blocks, block, stream
+void do_block_tree_attn(PyObject* const* a) {
+    cb_ctx* c = ctx_of(a[0]);
+    const Shape s = shape_of(a[1]);
+    const auto bf = at::kBFloat16;
+    const char *rows = "[batch, max_nodes, n_q_heads, head_dim]", *keys = "[batch, max_nodes, n_kv_heads, head_dim]";
+    cb_attn_args x = {};
+    x.q = arg(s, a[2], "q", bf, {s.B, s.T, s.Hq, s.D}, rows).p;
+    const Cache k = cache_of(s, a[3], a[4], a[5]);
+    x.k_pool = k.k; x.v_pool = k.v; x.block_table = k.table; x.max_pages = k.max_pages; x.num_pages = k.num_pages;
+    x.ctx_len = static_cast<int32_t*>(arg(s, a[6], "ctx_len", at::kInt, {s.B}, "[batch]").p);
+    x.k_tree = arg(s, a[7], "k_tree", bf, {s.B, s.T, s.Hkv, s.D}, keys).p;
+    x.v_tree = arg(s, a[8], "v_tree", bf, {s.B, s.T, s.Hkv, s.D}, keys).p;
+    x.tree_mask = static_cast<uint32_t*>(arg(s, a[9], "tree_mask", at::kInt, {s.B, s.T, (s.T + 31) / 32}, "[batch, max_nodes, words]").p);
+    x.n_nodes = static_cast<int32_t*>(arg(s, a[10], "n_nodes", at::kInt, {s.B}, "[batch]").p);
+    x.out = arg(s, a[11], "out", bf, {s.B, s.T, s.Hq, s.D}, rows).p;
+    x.lse = opt<float>(s, a[12], "lse", at::kFloat, {s.B, s.Hq, s.T}, "[batch, n_q_heads, max_nodes]");
+    x.max_ctx = int_of(a[13], "max_ctx");
+    x.scale = float_of(a[14]);
+    int32_t n_select;
+    const int32_t* blocks = blocks_of(s, a[15], &n_select);
+    const int32_t block = int_of(a[16], "block");
+    const OnDevice on(s, a[17]);
+    call("cb_block_tree_attn", [&] { return g_lib.block_tree_attn(c, &x, blocks, block, n_select, on.stream); });
 }
 // The outputs of log probabilities: a dictionary with logprobs and entropy, and the alternatives where there are any.
 void likely_of(const Shape& s, PyObject* res, PyObject* top, bool accept, int64_t n, cb_logprobs_args* x) {
@@ -492,7 +639,9 @@ PyObject* set_library(PyObject*, PyObject* args) {
           take("cb_update_draft_tree", &l.update_draft_tree) && take("cb_tree_attn", &l.tree_attn) && take("cb_accept", &l.accept) &&
           take("cb_accept_update_draft_tree", &l.accept_update_draft_tree) && take("cb_kv_commit", &l.kv_commit) && take("cb_chunk_append", &l.chunk_append) &&
           take("cb_chunk_attn", &l.chunk_attn) && take("cb_tree_rope", &l.tree_rope) && take("cb_logprobs", &l.logprobs) &&
-          take("cb_accept_logprobs", &l.accept_logprobs) && take("cb_status_str", &l.status_str)))
+          take("cb_accept_logprobs", &l.accept_logprobs) && take("cb_pages_assign", &l.pages_assign) && take("cb_slot_map", &l.slot_map) &&
+          take("cb_block_summary", &l.block_summary) && take("cb_block_select", &l.block_select) && take("cb_block_attn", &l.block_attn) &&
+          take("cb_block_tree_attn", &l.block_tree_attn) && take("cb_status_str", &l.status_str)))
         return nullptr;
     g_lib = l;
     Py_INCREF(err);
@@ -507,7 +656,9 @@ PyMethodDef g_methods[] = {
     CB_FAST("update_draft_tree", 6, do_update_draft), CB_FAST("accept", 6, do_accept), CB_FAST("accept_update_draft_tree", 8, do_accept_update_draft),
     CB_FAST("tree_attn", 15, do_attn), CB_FAST("kv_commit", 10, do_kv_commit), CB_FAST("chunk_append", 17, do_chunk_append),
     CB_FAST("tree_rope", 16, do_tree_rope), CB_FAST("chunk_attn", 14, do_chunk_attn), CB_FAST("logprobs", 8, do_logprobs),
-    CB_FAST("accept_logprobs", 7, do_accept_logprobs), {nullptr, nullptr, 0, nullptr}};
+    CB_FAST("accept_logprobs", 7, do_accept_logprobs), CB_FAST("pages_assign", 8, do_pages_assign), CB_FAST("slot_map", 9, do_slot_map),
+    CB_FAST("block_summary", 10, do_block_summary), CB_FAST("block_select", 17, do_block_select), CB_FAST("block_attn", 16, do_block_attn),
+    CB_FAST("block_tree_attn", 18, do_block_tree_attn), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -1,0 +1,23 @@
+// Attention over selected blocks: what its kernels share.
+#pragma once
+#include "cb_common.cuh"
+
+// The lists that attention over selected blocks reads: per sequence and kv head n_select numbers of blocks of 1 << shift tokens.
+struct CbBlockLists {
+    const int32_t* blocks;    // [batch, Hkv, n_select]; null: all of the context, no lists
+    int n_select, shift;
+};
+// A sequence of ctx cached tokens as its rows see it: the selected blocks one behind the other, and what follows the context behind them.  All blocks but
+// the newest, which is the last one of every list, are full, so that the number of visible tokens is the same for all heads.
+__host__ __device__ __forceinline__ int cb_blocks_of(int ctx, int shift) { return (int)(((long long)ctx + (1ll << shift) - 1) >> shift); }
+__host__ __device__ __forceinline__ int cb_seen(const CbBlockLists& l, int ctx) {
+    const int nb = cb_blocks_of(ctx, l.shift);
+    return nb > l.n_select ? ctx - ((nb - l.n_select) << l.shift) : ctx;
+}
+// Column of the block table for the i-th page that (b, kv head) sees, nb the blocks of the context; -1: none.
+__device__ __forceinline__ int cb_page_column(const CbBlockLists& l, int b, int Hkv, int kh, int nb, int i) {
+    const int per = l.shift - 4, at = i >> per, ns = min(nb, l.n_select);
+    if (at >= ns) return (nb << per) + i - (ns << per);       // behind the context: the chunk's own tokens
+    const int block = l.blocks[((size_t)b * Hkv + kh) * l.n_select + at];
+    return block >= 0 && block < nb ? (block << per) + (i & ((1 << per) - 1)) : -1;
+}

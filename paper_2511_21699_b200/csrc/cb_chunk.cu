@@ -73,16 +73,16 @@ __global__ void __launch_bounds__(32 * kWarps) cb_chunk_cc_kernel(const CbChunkP
 
 }  // namespace
 
-extern "C" cb_status cb_chunk_attn(cb_ctx* ctx, const cb_chunk_attn_args* a, void* stream) {
+cb_status cb_chunk_params(const cb_ctx* ctx, const cb_chunk_attn_args* a, CbChunkParams* out) {
     CB_CHECK_ARG(ctx && a);
     CB_CHECK_ARG(a->q && a->k_pool && a->v_pool && a->block_table && a->q_start && a->ctx_len && a->out && a->out != a->q);
     CB_CHECK_ARG(a->n_rows >= 0 && a->max_pages >= 1 && a->num_pages >= 1 && a->max_chunk >= 0 && a->max_ctx >= 0);
     const uintptr_t al = (uintptr_t)a->q | (uintptr_t)a->k_pool | (uintptr_t)a->v_pool | (uintptr_t)a->out;
     CB_CHECK_ARG((al & 15) == 0 && ((uintptr_t)a->lse & 3) == 0);
     CB_CHECK_ARG(a->scale >= 0.f && a->scale < INFINITY);     // (the kernels' running maximum is of scores times a positive number)
-    if (a->n_rows == 0) return CB_OK;
     const cb_config& c = ctx->cfg;
-    CbChunkParams p = {};
+    CbChunkParams& p = *out;
+    p = {};
     p.q = (const __nv_bfloat16*)a->q; p.k_pool = (const __nv_bfloat16*)a->k_pool; p.v_pool = (const __nv_bfloat16*)a->v_pool;
     p.block_table = a->block_table; p.q_start = a->q_start; p.ctx_len = a->ctx_len;
     p.out = (__nv_bfloat16*)a->out; p.lse = a->lse;
@@ -94,6 +94,14 @@ extern "C" cb_status cb_chunk_attn(cb_ctx* ctx, const cb_chunk_attn_args* a, voi
     const float scale = a->scale > 0.f ? a->scale : 1.0f / sqrtf((float)c.head_dim);
     p.scale_log2 = scale * 1.4426950408889634f;
     p.status = ctx->d_status;
+    return CB_OK;
+}
+
+extern "C" cb_status cb_chunk_attn(cb_ctx* ctx, const cb_chunk_attn_args* a, void* stream) {
+    CbChunkParams p;
+    const cb_status e = cb_chunk_params(ctx, a, &p);
+    if (e != CB_OK || a->n_rows == 0) return e;
+    const cb_config& c = ctx->cfg;
     cudaStream_t st = (cudaStream_t)stream;
     if (!(c.flags & CB_FLAG_ATTN_CUDA_CORES)) return cb_chunk_launch_tensor(ctx, p, st);
     const long long blocks = ((long long)p.n_rows * p.Hq + (p.B + 31) / 32 + kWarps - 1) / kWarps;

@@ -57,4 +57,6 @@ __device__ __forceinline__ CbChunkSeq cb_chunk_seq(const CbChunkParams& p, int b
     return s;
 }
 
+// Checks the arguments of chunk attention and fills in what its kernels are given (but for the tensor-core kernel's split).
+cb_status cb_chunk_params(const cb_ctx* ctx, const cb_chunk_attn_args* a, CbChunkParams* p);
 cb_status cb_chunk_launch_tensor(cb_ctx* ctx, const CbChunkParams& p, cudaStream_t st);

@@ -13,20 +13,10 @@ namespace {
 
 constexpr int kWarps = 4;
 
-// What the plain kernel is given; a tree's rows are b * T + node.
-struct PlainParams {
-    CbChunkParams c;
-    CbBlockLists l;
-    const __nv_bfloat16 *k_tree, *v_tree;
-    const uint32_t* mask;
-    const int32_t* n_nodes;
-    int T, W;
-};
-
-template <int D, bool TREE>
-__global__ void __launch_bounds__(32 * kWarps) cb_block_cc_kernel(const PlainParams x) {
+template <int D, typename P>
+__global__ void __launch_bounds__(32 * kWarps) cb_block_cc_kernel(const P p) {
     constexpr int C = D / 32;
-    const CbChunkParams& p = x.c;
+    constexpr bool TREE = P::kMode == 2;
     const int lane = threadIdx.x & 31;
     const long long item = (long long)blockIdx.x * kWarps + (threadIdx.x >> 5);
     const long long rows = (long long)p.n_rows * p.Hq;
@@ -38,37 +28,41 @@ __global__ void __launch_bounds__(32 * kWarps) cb_block_cc_kernel(const PlainPar
     }
     const int row = (int)(item / p.Hq), h = (int)(item % p.Hq), kh = h / p.G;
     int b, ctx, i, own;                                       // own: new tokens (nodes) that the row may see
-    if (TREE) {
-        b = row / x.T; i = row % x.T;
-        ctx = min(max(p.ctx_len[b], 0), p.max_keys);
-        own = min(max(x.n_nodes[b], 0), x.T);
+    if constexpr (TREE) {
+        b = row / p.T; i = row % p.T;
+        ctx = cb_tree_ctx(p, b);
+        own = min(max(p.n_nodes[b], 0), p.T);
         if (i >= own) {                                       // padding
             for (int c = 0; c < C; ++c) p.out[((size_t)row * p.Hq + h) * D + lane + 32 * c] = __float2bfloat16_rn(0.f);
-            if (p.lse && lane == 0) p.lse[((size_t)b * p.Hq + h) * x.T + i] = 0.f;
+            if (p.lse && lane == 0) p.lse[((size_t)b * p.Hq + h) * p.T + i] = 0.f;
             return;
         }
     } else {
         int q0, q1;
         b = cb_find_sequence(p.q_start, p.B, row, lane, p.ctx_len, &q0, &q1, &ctx);
         if (b < 0) return;
-        const CbChunkSeq s = cb_chunk_seq(p, b);
+        const CbChunkSeq s = cb_chunk_seq(static_cast<const CbChunkParams&>(p), b);   // (its context as it is)
         if (s.n == 0 || row - s.row0 >= s.n) return;
         ctx = s.ctx; i = row - s.row0; own = i + 1;
     }
-    const int nb = cb_blocks_of(ctx, x.l.shift), seen = cb_seen(x.l, ctx), keys = seen + own;
+    const int nb = cb_blocks_of(ctx, p.l.shift), seen = cb_seen(p.l, ctx), keys = seen + own;
     const __nv_bfloat16* q = p.q + ((size_t)row * p.Hq + h) * D;
     float m = -INFINITY, l = 0.f, acc[C] = {};
     for (int k0 = 0; k0 < keys; k0 += 32) {
         const int key = k0 + lane;
         const __nv_bfloat16 *kp = nullptr, *vp = nullptr;     // this lane's key; null: none, or a page outside the pool
         bool vis = key < keys;
-        if (vis && TREE && key >= seen) {
-            const int j = key - seen;
-            vis = (x.mask[((size_t)b * x.T + i) * x.W + (j >> 5)] >> (j & 31)) & 1u;
-            kp = x.k_tree + (((size_t)b * x.T + j) * p.Hkv + kh) * D;
-            vp = x.v_tree + (((size_t)b * x.T + j) * p.Hkv + kh) * D;
-        } else if (vis) {
-            const int col = cb_page_column(x.l, b, p.Hkv, kh, nb, key / p.P);
+        const bool node = TREE && vis && key >= seen;
+        if constexpr (TREE) {
+            if (node) {
+                const int j = key - seen;
+                vis = (p.mask[((size_t)b * p.T + i) * p.W + (j >> 5)] >> (j & 31)) & 1u;
+                kp = p.k_tree + (((size_t)b * p.T + j) * p.Hkv + kh) * D;
+                vp = p.v_tree + (((size_t)b * p.T + j) * p.Hkv + kh) * D;
+            }
+        }
+        if (vis && !node) {
+            const int col = cb_page_column(p.l, b, p.Hkv, kh, nb, key / p.P);
             const int page = col >= 0 && col < p.max_pages ? p.block_table[(size_t)b * p.max_pages + col] : -1;
             if (page >= 0 && page < p.num_pages) {
                 const size_t at = (((size_t)page * p.P + key % p.P) * p.Hkv + kh) * D;
@@ -106,7 +100,7 @@ __global__ void __launch_bounds__(32 * kWarps) cb_block_cc_kernel(const PlainPar
     for (int c = 0; c < C; ++c) p.out[((size_t)row * p.Hq + h) * D + lane + 32 * c] = __float2bfloat16_rn(acc[c] * inv);
     if (p.lse && lane == 0) {
         const float e = l > 0.f ? (m + log2f(l)) * 0.6931471805599453f : 0.f;
-        if (TREE) p.lse[((size_t)b * p.Hq + h) * x.T + i] = e;
+        if constexpr (TREE) p.lse[((size_t)b * p.Hq + h) * p.T + i] = e;
         else p.lse[(size_t)row * p.Hq + h] = e;
     }
 }
@@ -115,13 +109,12 @@ bool lists_ok(const int32_t* blocks, int32_t block, int32_t n_select) {
     return blocks && (block == 16 || block == 32 || block == 64 || block == 128) && n_select >= 1 && n_select <= CB_MAX_SELECT;
 }
 
-template <bool TREE>
-cb_status launch_plain(cb_ctx*, const PlainParams& x, cudaStream_t st) {
-    const CbChunkParams& p = x.c;
+template <typename P>
+cb_status launch_plain(const P& p, cudaStream_t st) {
     const long long blocks = ((long long)p.n_rows * p.Hq + (p.B + 31) / 32 + kWarps - 1) / kWarps;
     if (blocks > 0x7FFFFFFFll) return CB_ERR_UNSUPPORTED;
-    if (p.D == 128) cb_block_cc_kernel<128, TREE><<<(unsigned)blocks, 32 * kWarps, 0, st>>>(x);
-    else cb_block_cc_kernel<64, TREE><<<(unsigned)blocks, 32 * kWarps, 0, st>>>(x);
+    if (p.D == 128) cb_block_cc_kernel<128><<<(unsigned)blocks, 32 * kWarps, 0, st>>>(p);
+    else cb_block_cc_kernel<64><<<(unsigned)blocks, 32 * kWarps, 0, st>>>(p);
     cb_count_launch(1);
     CB_CUDA(cudaGetLastError());
     return CB_OK;
@@ -131,12 +124,12 @@ cb_status launch_plain(cb_ctx*, const PlainParams& x, cudaStream_t st) {
 
 extern "C" cb_status cb_block_attn(cb_ctx* ctx, const cb_chunk_attn_args* a, const int32_t* blocks, int32_t block, int32_t n_select, void* stream) {
     CB_CHECK_ARG(ctx && a && lists_ok(blocks, block, n_select));
-    CbChunkParams p;
+    CbListParams p = {};
     const cb_status e = cb_chunk_params(ctx, a, &p);
     if (e != CB_OK || a->n_rows == 0) return e;
-    PlainParams x = {};
-    x.c = p; x.l = {blocks, n_select, __builtin_ctz((unsigned)block)};
-    return launch_plain<false>(ctx, x, (cudaStream_t)stream);
+    p.l = {blocks, n_select, __builtin_ctz((unsigned)block)};
+    cudaStream_t st = (cudaStream_t)stream;
+    return ctx->cfg.flags & CB_FLAG_ATTN_CUDA_CORES ? launch_plain(p, st) : cb_block_launch_tensor(ctx, p, st);
 }
 
 extern "C" cb_status cb_block_tree_attn(cb_ctx* ctx, const cb_attn_args* a, const int32_t* blocks, int32_t block, int32_t n_select, void* stream) {
@@ -148,8 +141,7 @@ extern "C" cb_status cb_block_tree_attn(cb_ctx* ctx, const cb_attn_args* a, cons
     CB_CHECK_ARG(a->scale >= 0.f && a->scale < INFINITY);
     const cb_config& c = ctx->cfg;
     if ((long long)c.batch * c.max_nodes > 0x7FFFFFFFll) return CB_ERR_UNSUPPORTED;
-    PlainParams x = {};
-    CbChunkParams& p = x.c;
+    CbListTreeParams p = {};
     p.q = (const __nv_bfloat16*)a->q; p.k_pool = (const __nv_bfloat16*)a->k_pool; p.v_pool = (const __nv_bfloat16*)a->v_pool;
     p.block_table = a->block_table; p.ctx_len = a->ctx_len; p.out = (__nv_bfloat16*)a->out; p.lse = a->lse;
     p.B = c.batch; p.Hq = c.n_q_heads; p.Hkv = c.n_kv_heads; p.G = c.n_q_heads / c.n_kv_heads; p.D = c.head_dim; p.P = c.page_size;
@@ -158,8 +150,9 @@ extern "C" cb_status cb_block_tree_attn(cb_ctx* ctx, const cb_attn_args* a, cons
     p.max_keys = (int)(a->max_ctx > 0 ? std::min<long long>(a->max_ctx, cap) : cap);
     p.scale_log2 = (a->scale > 0.f ? a->scale : 1.0f / sqrtf((float)c.head_dim)) * 1.4426950408889634f;
     p.status = ctx->d_status;
-    x.k_tree = (const __nv_bfloat16*)a->k_tree; x.v_tree = (const __nv_bfloat16*)a->v_tree; x.mask = a->tree_mask; x.n_nodes = a->n_nodes;
-    x.T = c.max_nodes; x.W = (c.max_nodes + 31) / 32;
-    x.l = {blocks, n_select, __builtin_ctz((unsigned)block)};
-    return launch_plain<true>(ctx, x, (cudaStream_t)stream);
+    p.k_tree = (const __nv_bfloat16*)a->k_tree; p.v_tree = (const __nv_bfloat16*)a->v_tree; p.mask = a->tree_mask; p.n_nodes = a->n_nodes;
+    p.T = c.max_nodes; p.W = (c.max_nodes + 31) / 32;
+    p.l = {blocks, n_select, __builtin_ctz((unsigned)block)};
+    cudaStream_t st = (cudaStream_t)stream;
+    return c.flags & CB_FLAG_ATTN_CUDA_CORES ? launch_plain(p, st) : cb_block_launch_tensor(ctx, p, st);
 }

@@ -1,6 +1,6 @@
 // Attention over selected blocks: what its kernels share.
 #pragma once
-#include "cb_common.cuh"
+#include "cb_chunk.cuh"
 
 // The lists that attention over selected blocks reads: per sequence and kv head n_select numbers of blocks of 1 << shift tokens.
 struct CbBlockLists {
@@ -21,3 +21,29 @@ __device__ __forceinline__ int cb_page_column(const CbBlockLists& l, int b, int 
     const int block = l.blocks[((size_t)b * Hkv + kh) * l.n_select + at];
     return block >= 0 && block < nb ? (block << per) + (i & ((1 << per) - 1)) : -1;
 }
+
+// What attention over selected blocks is given: of chunks, and of draft trees (rows b * T + node, max_chunk = T).
+struct CbListParams : CbChunkParams {
+    static constexpr int kMode = 1;
+    CbBlockLists l;
+};
+struct CbListTreeParams : CbListParams {
+    static constexpr int kMode = 2;
+    const __nv_bfloat16 *k_tree, *v_tree;
+    const uint32_t* mask;
+    const int32_t* n_nodes;
+    int T, W;
+};
+// Their sequences, the context as the rows see it.
+__device__ __forceinline__ CbChunkSeq cb_chunk_seq(const CbListParams& p, int b) {
+    CbChunkSeq s = cb_chunk_seq(static_cast<const CbChunkParams&>(p), b);
+    if (s.n > 0) s.ctx = cb_seen(p.l, s.ctx);
+    return s;
+}
+__device__ __forceinline__ int cb_tree_ctx(const CbListTreeParams& p, int b) { return min(max(p.ctx_len[b], 0), p.max_keys); }
+__device__ __forceinline__ CbChunkSeq cb_chunk_seq(const CbListTreeParams& p, int b) {
+    return {b * p.T, min(max(p.n_nodes[b], 0), p.T), cb_seen(p.l, cb_tree_ctx(p, b)), 0};
+}
+
+cb_status cb_block_launch_tensor(cb_ctx* ctx, const CbListParams& p, cudaStream_t st);
+cb_status cb_block_launch_tensor(cb_ctx* ctx, const CbListTreeParams& p, cudaStream_t st);

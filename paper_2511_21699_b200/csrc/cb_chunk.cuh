@@ -25,6 +25,7 @@ __device__ __forceinline__ int cb_find_sequence(const int32_t* q_start, int B, i
 
 // What attention of packed chunks is given.
 struct CbChunkParams {
+    static constexpr int kMode = 0;   // 0: all of the context; 1, 2: selected blocks of it, for chunks and for trees (cb_blocks.cuh)
     const __nv_bfloat16 *q, *k_pool, *v_pool;
     const int32_t *block_table, *q_start, *ctx_len;
     __nv_bfloat16* out;

@@ -63,13 +63,15 @@ struct CbChunkCuts {
     }
 };
 
-struct CbChunkShape {
+// TREE: the rows are the nodes of a draft tree, whose keys are a tile of their own behind the context's, the same for all rows.
+template <bool TREE>
+struct CbChunkShapeT {
     int row0 = 0, n = 0, ctx = 0, error = 0;
     int mtn = 0, RG = 0, tg = 0;   // row tiles, row groups, tokens per row group
     int w1 = 0, w2 = 0, d1 = 0, d2 = 0;
     bool one = false;
     __device__ __forceinline__ int end(int rg) const { return ctx + min(n, (rg + 1) * tg); }                 // keys that row group rg sees
-    __device__ __forceinline__ int tiles(int rg) const { return (end(rg) + CB_KT - 1) / CB_KT; }
+    __device__ __forceinline__ int tiles(int rg) const { return TREE ? (ctx + CB_KT - 1) / CB_KT + 1 : (end(rg) + CB_KT - 1) / CB_KT; }
     __device__ __forceinline__ bool two_rows(int rg) const { return !one && mtn - 2 * rg >= 2; }
     __device__ __forceinline__ int wt(int rg) const { return two_rows(rg) ? w2 : w1; }
     __device__ __forceinline__ int ov(int rg) const { return two_rows(rg) ? 3 * w2 : 2 * w1; }
@@ -79,14 +81,19 @@ struct CbChunkShape {
     __device__ __forceinline__ long long before(int r) const {
         if (r <= 0) return 0;
         const int k = min(r, RG - 1);
+        if (TREE) return (long long)k * unit(0) + (r == RG ? unit(RG - 1) : 0);
         return w2 * (cb_floor_sum(k, tg, ctx + tg + CB_KT - 1) + 3ll * k) + (r == RG ? unit(RG - 1) : 0);
     }
     __device__ __forceinline__ long long weight(int Hkv) const { return RG > 0 ? Hkv * before(RG) : 0; }
 };
+using CbChunkShape = CbChunkShapeT<false>;
+// The shape of what attention is given as P (CbChunkParams and what is derived from it, by its kMode).
+template <typename P> using CbShapeOf = CbChunkShapeT<P::kMode == 2>;
 
-__device__ __forceinline__ CbChunkShape cb_chunk_shape(const CbChunkParams& p, int b) {
+template <typename P>
+__device__ __forceinline__ CbShapeOf<P> cb_chunk_shape(const P& p, int b) {
     const CbChunkSeq q = cb_chunk_seq(p, b);
-    CbChunkShape s;
+    CbShapeOf<P> s;
     s.row0 = q.row0; s.n = q.n; s.ctx = q.ctx; s.error = q.error;
     s.mtn = (q.n + p.NPT - 1) / p.NPT;
     s.one = p.one != 0;
@@ -98,11 +105,13 @@ __device__ __forceinline__ CbChunkShape cb_chunk_shape(const CbChunkParams& p, i
 
 // Walks the units of the range [g, g1).
 struct CbChunkUnit { int b, kh, rg, t0, t1; long long first; };   // first: position of the unit's first tile's deciding position
-struct CbChunkWalker {
+template <bool TREE>
+struct CbChunkWalkerT {
     long long g, g1, pos;     // pos: where the current unit starts
     int b, rg, kh;
-    CbChunkShape s;
-    __device__ __forceinline__ bool next(const CbChunkParams& p, CbChunkUnit* u) {
+    CbChunkShapeT<TREE> s;
+    template <typename P>
+    __device__ __forceinline__ bool next(const P& p, CbChunkUnit* u) {
         while (g < g1) {
             if (rg == s.RG) {                                 // on to the next sequence that has any
                 rg = 0;
@@ -127,7 +136,8 @@ struct CbChunkWalker {
     }
     // The same with two whole units of one row tile at a time, of neighbouring heads, where the range holds the second one's tiles as well: a chain
     // each, so that what lies between two units (some 7 k cycles of a unit of one tile) is paid once for both.
-    __device__ __forceinline__ bool next_pair(const CbChunkParams& p, CbChunkUnit* u, bool* heads) {
+    template <typename P>
+    __device__ __forceinline__ bool next_pair(const P& p, CbChunkUnit* u, bool* heads) {
         *heads = false;
         if (!next(p, u)) return false;
         const int tiles = s.tiles(u->rg);
@@ -143,16 +153,18 @@ struct CbChunkWalker {
         return true;
     }
 };
+using CbChunkWalker = CbChunkWalkerT<false>;
 
 // This CTA's range and the walker at its start, by a whole warp (every lane gets both), and the cuts.  *error: what this lane found wrong with a
 // sequence, or 0.
-__device__ __forceinline__ void cb_chunk_range(const CbChunkParams& p, int cta, int lane, CbChunkWalker* w, CbChunkCuts* cuts, int* error) {
-    auto shape = [&](int b) { return b < p.B ? cb_chunk_shape(p, b) : CbChunkShape{}; };
-    CbChunkShape s = shape(lane);
+template <typename P>
+__device__ __forceinline__ void cb_chunk_range(const P& p, int cta, int lane, CbChunkWalkerT<P::kMode == 2>* w, CbChunkCuts* cuts, int* error) {
+    auto shape = [&](int b) { return b < p.B ? cb_chunk_shape(p, b) : CbShapeOf<P>{}; };
+    CbShapeOf<P> s = shape(lane);
     long long own = s.weight(p.Hkv), tot = own;
     int err = s.error;
     for (int b = 32 + lane; b - lane < p.B; b += 32) {
-        const CbChunkShape t = shape(b);
+        const CbShapeOf<P> t = shape(b);
         if (t.error) err = t.error;
         tot += t.weight(p.Hkv);
     }
@@ -214,7 +226,8 @@ __device__ __forceinline__ void cb_chunk_range(const CbChunkParams& p, int cta, 
 // Launches of few units of one row tile (single tokens of a small batch) are not cut into ranges: unit u = (sequence, kv head) has CTAs
 // u cs .. u cs + cs - 1, which take equal parts of its tiles.  A CTA then needs one sequence's lengths and next to no arithmetic before its
 // first copy, and no CTA has more than one unit to see to.
-__device__ __forceinline__ bool cb_chunk_share(const CbChunkParams& p, int b, int kh, int rank, CbChunkUnit* u, CbChunkShape* s, int* ctas) {
+template <typename P>
+__device__ __forceinline__ bool cb_chunk_share(const P& p, int b, int kh, int rank, CbChunkUnit* u, CbShapeOf<P>* s, int* ctas) {
     u->b = b; u->kh = kh; u->rg = 0;
     *s = cb_chunk_shape(p, b);
     if (s->RG == 0) return false;

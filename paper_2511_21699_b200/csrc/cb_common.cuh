@@ -153,6 +153,19 @@ inline cudaError_t cb_launch_pdl(void (*kernel)(KArgs...), dim3 grid, dim3 block
     cfg.attrs = at; cfg.numAttrs = 1;
     return cudaLaunchKernelEx(&cfg, kernel, std::forward<Args>(args)...);
 }
+// The same with the grid cut into clusters of `ctas` blocks.
+template <typename... KArgs, typename... Args>
+inline cudaError_t cb_launch_clusters(void (*kernel)(KArgs...), unsigned grid, unsigned ctas, unsigned block, size_t smem, cudaStream_t st, Args&&... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid); cfg.blockDim = dim3(block); cfg.dynamicSmemBytes = smem; cfg.stream = st;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = ctas; at[1].val.clusterDim.y = 1; at[1].val.clusterDim.z = 1;
+    cfg.attrs = at; cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, kernel, std::forward<Args>(args)...);
+}
 // Lets a kernel's blocks have `bytes` of dynamic shared memory.  Unasked a block gets 48 KB, its static part included.  *have: what it
 // may have so far, per device and kernel (0: not asked yet); the caller guards it.
 template <typename Kernel>

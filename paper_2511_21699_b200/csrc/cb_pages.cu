@@ -134,18 +134,10 @@ extern "C" cb_status cb_pages_assign(cb_ctx* ctx, const int32_t* want_len, int32
     if (c.batch > CB_MAX_ASSIGN) return CB_ERR_UNSUPPORTED;
     const size_t smem = (size_t)c.batch * 8;
     if (smem > 40 * 1024) CB_CUDA(cudaFuncSetAttribute(cb_pages_assign_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, CB_MAX_ASSIGN * 8));
-    cudaLaunchConfig_t cfg = {};
     // Eight CTAs where a call may have many moves (how many is known on the device only).
     const unsigned ctas = (long long)c.batch * max_pages > 8192 ? 8 : 1;
-    cfg.gridDim = dim3(ctas); cfg.blockDim = dim3(kPageThreads); cfg.dynamicSmemBytes = smem; cfg.stream = (cudaStream_t)stream;
-    cudaLaunchAttribute at[2];
-    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[0].val.programmaticStreamSerializationAllowed = 1;
-    at[1].id = cudaLaunchAttributeClusterDimension;
-    at[1].val.clusterDim.x = ctas; at[1].val.clusterDim.y = 1; at[1].val.clusterDim.z = 1;
-    cfg.attrs = at; cfg.numAttrs = 2;
-    CB_CUDA(cudaLaunchKernelEx(&cfg, cb_pages_assign_kernel, (int)c.batch, (int)c.page_size, (int)max_pages, (int)num_pages, want_len, block_table, held, free_pages,
-                               n_free, ctx->d_status));
+    CB_CUDA(cb_launch_clusters(cb_pages_assign_kernel, ctas, ctas, kPageThreads, smem, (cudaStream_t)stream, (int)c.batch, (int)c.page_size, (int)max_pages,
+                               (int)num_pages, want_len, block_table, held, free_pages, n_free, ctx->d_status));
     cb_count_launch(1);
     return CB_OK;
 }

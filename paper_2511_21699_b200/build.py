@@ -13,7 +13,7 @@ SO = os.path.join(HERE, "libcacheback.so")
 SO_DEBUG = os.path.join(HERE, "libcacheback_debug.so")
 SO_BINDING = os.path.join(HERE, "_binding.so")
 SOURCES = ["cb_api.cu", "cb_table.cu", "cb_accept.cu", "cb_kv.cu", "cb_branches.cu", "cb_frozen.cu", "cb_frozen_build.cu", "cb_attn.cu", "cb_attn_tc.cu", "cb_rope.cu",
-           "cb_logprobs.cu", "cb_chunk.cu", "cb_chunk_tc.cu", "cb_pages.cu", "cb_blocks.cu", "cb_block_attn.cu", "cb_block_tc.cu", "cb_select_tc.cu"]
+           "cb_logprobs.cu", "cb_chunk.cu", "cb_chunk_tc.cu", "cb_pages.cu", "cb_blocks.cu", "cb_block_attn.cu", "cb_block_tc.cu", "cb_select_tc.cu", "cb_block_token.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "-I", os.path.join(ROOT, "include"), "-I", CSRC]
 

@@ -129,7 +129,8 @@ extern "C" cb_status cb_block_attn(cb_ctx* ctx, const cb_chunk_attn_args* a, con
     if (e != CB_OK || a->n_rows == 0) return e;
     p.l = {blocks, n_select, __builtin_ctz((unsigned)block)};
     cudaStream_t st = (cudaStream_t)stream;
-    return ctx->cfg.flags & CB_FLAG_ATTN_CUDA_CORES ? launch_plain(p, st) : cb_block_launch_tensor(ctx, p, st);
+    if (ctx->cfg.flags & CB_FLAG_ATTN_CUDA_CORES) return launch_plain(p, st);
+    return (long long)p.max_chunk * p.G <= 16 ? cb_block_launch_token(ctx, p, st) : cb_block_launch_tensor(ctx, p, st);
 }
 
 extern "C" cb_status cb_block_tree_attn(cb_ctx* ctx, const cb_attn_args* a, const int32_t* blocks, int32_t block, int32_t n_select, void* stream) {

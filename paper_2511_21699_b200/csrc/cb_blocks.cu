@@ -123,14 +123,14 @@ __device__ __forceinline__ void mma_s8(int* c, uint32_t a0, uint32_t a1, uint32_
 // pipe is 2% busy).  A dot product does not mind the order of its terms, so the k-th step takes, of the 16-byte pieces that lane t of a row's four lanes holds
 // (piece t, and with 128 dims piece t + 4), the words that make a fragment: both sides come from memory in 16-byte pieces and go into the products as they are.
 template <int D, int NT>
-__global__ void __launch_bounds__(kFewThreads, 4) cb_select_few_kernel(const CbSelectParams p) {
+__global__ void __launch_bounds__(kFewThreads, 3) cb_select_few_kernel(const CbSelectParams p) {
     constexpr int W = D / 16, L = D / 16;                     // words of a row that a lane holds; lanes that copy a row
     extern __shared__ __align__(16) uint32_t s_dyn[];
     __shared__ __align__(16) uint32_t s_scratch[cb_pick_words<kFewThreads>];
     uint32_t* const s_key = s_dyn;
     CB_PDL_ENTRY();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, gid = lane >> 2, tig = lane & 3;
-    uint8_t* const s_rows = reinterpret_cast<uint8_t*>(s_dyn + p.key_words) + warp * (32 * D);
+    uint8_t* const s_rows = reinterpret_cast<uint8_t*>(s_dyn + p.key_words) + warp * (2 * 32 * D);
     uint32_t rank, ranks;
     asm("mov.u32 %0, %cluster_ctarank;" : "=r"(rank));
     asm("mov.u32 %0, %cluster_nctarank;" : "=r"(ranks));
@@ -148,23 +148,25 @@ __global__ void __launch_bounds__(kFewThreads, 4) cb_select_few_kernel(const CbS
     for (int k = tid; k < cb_pick_words<kFewThreads>; k += kFewThreads) s_scratch[k] = 0u;
     if (ranks > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
     // Row i's piece c lies at piece c ^ (i & 1) * 4 (128 dims), so that eight lanes that read two rows meet no bank twice.
-    auto piece = [&](int i, int c) { return s_rows + i * D + ((D == 128 ? c ^ ((i & 1) << 2) : c) << 4); };
-    float scale = 0.f;
-    bool good = true;
-    auto load_rows = [&](int base) {
-        good = base + lane >= nb || (page >= 0 && page < p.num_pages);
-        const int at = good && base + lane < nb ? page : 0;
+    auto piece = [&](int half, int i, int c) { return s_rows + half * (32 * D) + i * D + ((D == 128 ? c ^ ((i & 1) << 2) : c) << 4); };
+    // The 32 blocks from base on into one half of the warp's rows; the next 32 are on their way while these are scored.
+    float scale = 0.f, scale_next = 0.f;
+    bool good = true, good_next = true;
+    auto load_rows = [&](int base, int half) {
+        good_next = base + lane >= nb || (page >= 0 && page < p.num_pages);
+        const int at = good_next && base + lane < nb ? page : 0;
 #pragma unroll
         for (int k = 0; k < L; ++k) {
             const int row = k * (32 / L) + lane / L, pg = __shfl_sync(CB_FULL, at, row);
             const int8_t* src = p.mean + ((size_t)pg * p.Hkv + u.kh) * D + lane % L * 16;
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(piece(row, lane % L))), "l"(src) : "memory");
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(piece(half, row, lane % L))), "l"(src) : "memory");
         }
-        scale = good ? __ldg(p.scale + (size_t)at * p.Hkv + u.kh) : 0.f;
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        scale_next = good_next ? __ldg(p.scale + (size_t)at * p.Hkv + u.kh) : 0.f;
         page = page_next;
         if (base + 2 * step < nb) page_next = page_of(base + 2 * step);
     };
-    if (start < nb) load_rows(start);
+    if (start < nb) load_rows(start, 0);
     // the queries: each one's pieces tig and tig + 4, whole numbers of a common scale; what there is less than 8 is filled up with the first
     uint32_t w[NT][W], top = 0;
     {
@@ -191,9 +193,15 @@ __global__ void __launch_bounds__(kFewThreads, 4) cb_select_few_kernel(const CbS
         key0 = cb_cluster_first(s_key);
         cb_cluster_wait();
     }
-    for (int base = start; base < nb; base += step) {
-        if (base != start) load_rows(base);
-        asm volatile("cp.async.wait_all;" ::: "memory");
+    int half = 0;
+    for (int base = start; base < nb; base += step, half ^= 1) {
+        good = good_next; scale = scale_next;
+        if (base + step < nb) {
+            load_rows(base + step, half ^ 1);
+            asm volatile("cp.async.wait_group 1;" ::: "memory");
+        } else {
+            asm volatile("cp.async.wait_group 0;" ::: "memory");
+        }
         __syncwarp();
         int mine = 0;                                         // the largest product of block base + lane
 #pragma unroll
@@ -203,7 +211,7 @@ __global__ void __launch_bounds__(kFewThreads, 4) cb_select_few_kernel(const CbS
             for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int c = 0; c < W / 4; ++c) {
-                    const uint4 x = *reinterpret_cast<const uint4*>(piece(g * 16 + h * 8 + gid, tig + 4 * c));
+                    const uint4 x = *reinterpret_cast<const uint4*>(piece(half, g * 16 + h * 8 + gid, tig + 4 * c));
                     a[h][4 * c] = x.x; a[h][4 * c + 1] = x.y; a[h][4 * c + 2] = x.z; a[h][4 * c + 3] = x.w;
                 }
             int best[2] = {INT32_MIN, INT32_MIN};
@@ -310,7 +318,7 @@ extern "C" cb_status cb_block_select(cb_ctx* ctx, const cb_block_select_args* a,
     int ctas = 1;
     while (ctas < 8 && (long long)p.B * p.Hkv * ctas * 2 <= ctx->num_sms && blocks > ctas * 128) ctas *= 2;
     if (nt == 0) return cb_select_launch_many(ctx, p, ctas, (cudaStream_t)stream);
-    const size_t smem = (size_t)p.key_words * 4 + (size_t)kFewThreads * c.head_dim;
+    const size_t smem = (size_t)p.key_words * 4 + (size_t)kFewThreads * 2 * c.head_dim;
     const auto launch = [&](auto kernel, int which) -> cb_status {
         {
             std::lock_guard<std::mutex> lock(g_mutex);

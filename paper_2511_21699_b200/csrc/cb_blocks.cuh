@@ -47,3 +47,5 @@ __device__ __forceinline__ CbChunkSeq cb_chunk_seq(const CbListTreeParams& p, in
 
 cb_status cb_block_launch_tensor(cb_ctx* ctx, const CbListParams& p, cudaStream_t st);
 cb_status cb_block_launch_tensor(cb_ctx* ctx, const CbListTreeParams& p, cudaStream_t st);
+// For units of up to 16 rows x heads: max_chunk * G <= 16.
+cb_status cb_block_launch_token(cb_ctx* ctx, const CbListParams& p, cudaStream_t st);

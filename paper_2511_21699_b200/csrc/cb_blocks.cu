@@ -27,37 +27,45 @@ struct SummaryParams {
     uint32_t* status;
 };
 
+// A bf16, the upper half of a word, as a double 2^-896 times as large: sign, exponent and mantissa moved to their places, which does for zero and
+// the smallest numbers too (infinity and NaN become numbers and are looked for apart).  A conversion has a quarter of these operations' rate, and the
+// kernel would wait for it.
+__device__ __forceinline__ double small_double(uint32_t upper) { return __hiloint2double(((int)upper >> 3) & 0x8FFFE000, 0); }
+constexpr double kSmallDouble = 0x1p896;
+
 template <int D, int S>
 __global__ void __launch_bounds__(kSumThreads) cb_block_summary_kernel(const SummaryParams p) {
     constexpr int HG = 256 / D, LH = D / 8, T = S / 8;        // heads of a CTA, lanes of a head, tokens of a warp
-    extern __shared__ int32_t s_sums[];                       // [2][B]
-    __shared__ long long s_scratch[66];
+    extern __shared__ uint32_t s_sums[];                      // [B]
+    __shared__ uint32_t s_scratch[kSumThreads / 32];
     __shared__ double s_part[8][256];                         // a warp's sums: channel lane * 8 + e at e * 32 + lane
     __shared__ unsigned long long s_top[8][HG];
     __shared__ __align__(16) int8_t s_out[256];
     CB_PDL_ENTRY();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     int error = 0;
-    cb_block_sums<kSumThreads>(p.B, s_sums, s_sums + p.B, s_scratch, [&](int b, int* blocks, int*) {
+    cb_block_sums<kSumThreads, 1>(p.B, s_sums, s_scratch, [&](int b, uint32_t* blocks) {
         const int lo = p.from[b], hi = p.to[b];
         if (lo >= hi) return;
         if (lo < 0) error = CB_ERR_INVALID_ARG;
         else if (hi > (long long)p.max_pages * p.P) error = CB_ERR_KV_FULL;
-        else *blocks = (hi - 1) / S - lo / S + 1;
+        else *blocks = (uint32_t)((hi - 1) / S - lo / S + 1);
     });
     if (error && blockIdx.x == 0) atomicCAS(p.status, 0u, (uint32_t)error);
     const int groups = (p.Hkv + HG - 1) / HG;
     const long long items = (long long)s_sums[p.B - 1] * groups;
     for (long long item = blockIdx.x; item < items; item += gridDim.x) {
-        const int at = (int)(item / groups), h0 = (int)(item % groups) * HG;
+        const uint32_t at = (uint32_t)(item / groups);
+        const int h0 = (int)(item - (long long)at * groups) * HG;
         const int b = cb_upper(s_sums, p.B, at);
-        const int blk = p.from[b] / S + at - (b > 0 ? s_sums[b - 1] : 0);
+        const int blk = p.from[b] / S + (int)(at - (b > 0 ? s_sums[b - 1] : 0u));
         const int n = min(S, p.to[b] - blk * S);
         const int32_t* pages = p.table + (size_t)b * p.max_pages + blk * (S / 16);
         const int page = lane < (n + 15) / 16 ? pages[lane] : 0;
         const bool good = __all_sync(CB_FULL, page >= 0 && page < p.num_pages);
         const int head = h0 + lane / LH;
         double sum[8] = {};
+        uint32_t bits = 0;                                    // largest magnitudes, as bits of bf16
         if (good) {
             uint4 v[T];
 #pragma unroll
@@ -72,22 +80,28 @@ __global__ void __launch_bounds__(kSumThreads) cb_block_summary_kernel(const Sum
                 const uint32_t w[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    sum[2 * e] += (double)__uint_as_float(w[e] << 16);
-                    sum[2 * e + 1] += (double)__uint_as_float(w[e] & 0xFFFF0000u);
+                    sum[2 * e] += small_double(w[e] << 16);
+                    sum[2 * e + 1] += small_double(w[e]);
+                    bits = __vmaxu2(bits, w[e] & 0x7FFF7FFFu);
                 }
             }
         }
 #pragma unroll
         for (int e = 0; e < 8; ++e) s_part[warp][e * 32 + lane] = sum[e];
+        unsigned long long top = max(bits & 0xFFFFu, bits >> 16) >= 0x7F80u ? 0x7FF0000000000000ull : 0ull;
+        if (lane % LH == 0) s_top[warp][lane / LH] = 0ull;
+        __syncwarp();
+        if (top) s_top[warp][lane / LH] = top;
         __syncthreads();
         double m = 0.0;
 #pragma unroll
-        for (int w = 0; w < 8; ++w) m += s_part[w][tid];
-        m = __ddiv_rn(m, (double)n);
-        // the largest magnitude as bits: NaN is above infinity there
-        unsigned long long top = (unsigned long long)__double_as_longlong(m) & 0x7FFFFFFFFFFFFFFFull;
+        for (int w = 0; w < 8; ++w) { m += s_part[w][tid]; top = max(top, s_top[w][lane / LH]); }
+        m = __ddiv_rn(__dmul_rn(m, kSmallDouble), (double)n);
+        // the largest magnitude, as bits
+        top = max(top, (unsigned long long)__double_as_longlong(m) & 0x7FFFFFFFFFFFFFFFull);
 #pragma unroll
         for (int o = LH / 2; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(CB_FULL, top, o));
+        __syncthreads();
         if (lane % LH == 0) s_top[warp][lane / LH] = top;
         __syncthreads();
 #pragma unroll
@@ -267,9 +281,9 @@ extern "C" cb_status cb_block_summary(cb_ctx* ctx, const cb_block_summary_args* 
     p.mean = a->k_mean; p.scale = a->k_scale;
     p.B = c.batch; p.Hkv = c.n_kv_heads; p.P = c.page_size; p.max_pages = a->max_pages; p.num_pages = a->num_pages;
     p.status = ctx->d_status;
-    const size_t smem = (size_t)c.batch * 8;
+    const size_t smem = (size_t)c.batch * 4;
     const auto launch = [&](auto kernel) -> cb_status {
-        if (smem > 16 * 1024) CB_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, CB_MAX_ASSIGN * 8));
+        if (smem > 16 * 1024) CB_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, CB_MAX_ASSIGN * 4));
         CB_CUDA(cb_launch_pdl(kernel, dim3(ctx->num_sms * 4), dim3(kSumThreads), smem, (cudaStream_t)stream, p));
         cb_count_launch(1);
         return CB_OK;

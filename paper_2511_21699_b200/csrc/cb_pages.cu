@@ -4,10 +4,13 @@
 // every CTA takes for itself.  The j-th page handed out is the j-th one given back or, behind those, the stack's from its top; it goes to the sequence whose
 // sum of needs passes j.  So all moves are independent: a thread finds both sequences of a move by two searches in shared memory.  Pages given back
 // that nobody takes are pushed above the old top, pages taken from the stack lie below it, rows that are read belong to sequences that shrink and rows
-// that are written to such that grow: no move touches what another one reads.  The CTAs form one cluster; held and n_free, which all of them read, are
-// written behind its barrier.
+// that are written to such that grow: no move touches what another one reads.  held and n_free, which all CTAs read, are written by the one that counted itself
+// last behind that.  How many moves there are is known on the device only: a table of up to 65,536 entries gets one CTA (a step's few moves: the count would cost
+// more than it shares), a larger one as many as it has 2,048 entries, one an SM at most.
 //
 // cb_slot_map.  A thread per row: the sequence by a search in the block's copy of q_start, then its length and page.
+#include <algorithm>
+
 #include "cb_scan.cuh"
 
 namespace {
@@ -15,54 +18,59 @@ namespace {
 constexpr int kPageThreads = 1024;
 
 __global__ void __launch_bounds__(kPageThreads) cb_pages_assign_kernel(int B, int P, int max_pages, int num_pages, const int32_t* __restrict__ want_len, int32_t* table,
-                                                                       int32_t* held, int32_t* stack, int32_t* n_free, uint32_t* status) {
-    extern __shared__ int32_t s_sums[];                       // [2][B]: needs, pages given back
-    __shared__ long long s_scratch[66];
-    int32_t *const s_need = s_sums, *const s_back = s_sums + B;
+                                                                       int32_t* held, int32_t* stack, int32_t* n_free, uint32_t* ticket, uint32_t* status) {
+    extern __shared__ uint32_t s_sums[];                      // [2][B]: needs, pages given back
+    __shared__ uint32_t s_scratch[2 * kPageThreads / 32];
+    __shared__ int s_last;
+    uint32_t *const s_need = s_sums, *const s_back = s_sums + B;
     CB_PDL_ENTRY();
     const int tid = threadIdx.x;
-    uint32_t rank, ranks;
-    asm("mov.u32 %0, %cluster_ctarank;" : "=r"(rank));
-    asm("mov.u32 %0, %cluster_nctarank;" : "=r"(ranks));
     const int free0 = n_free[0];
     int error = free0 < 0 || free0 > num_pages ? CB_ERR_INVALID_ARG : 0;
     const bool stack_ok = error == 0;
     // pages that the sequence is to hold; -1: it is left alone
+    auto pages_of = [&](int w) { return w / P + (w % P != 0); };
     auto target = [&](int b, int h, int* why) {
         const int w = want_len[b];
         if (w < 0 || h < 0 || h > max_pages) { *why = CB_ERR_INVALID_ARG; return -1; }
-        const int t = w / P + (w % P != 0);
+        const int t = pages_of(w);
         if (t > max_pages) { *why = CB_ERR_KV_FULL; return -1; }
         return t;
     };
-    cb_block_sums<kPageThreads>(B, s_need, s_back, s_scratch, [&](int b, int* need, int* back) {
+    cb_block_sums<kPageThreads, 2>(B, s_sums, s_scratch, [&](int b, uint32_t* c) {
         const int h = held[b];
         const int t = target(b, h, &error);
-        if (t >= 0) { *need = max(t - h, 0); *back = max(h - t, 0); }
+        if (t >= 0) { c[0] = min((uint32_t)max(t - h, 0), CB_SUM_CAP); c[1] = min((uint32_t)max(h - t, 0), CB_SUM_CAP); }
     });
-    const long long given = s_back[B - 1], there = (long long)free0 + given;
-    const bool ok = stack_ok && there <= num_pages;
-    // needs that are met: the largest sum that does not exceed what is there
-    const int met = ok ? cb_upper(s_need, B, (int)min(there, 0x7FFFFFFEll)) : 0;
-    const int taken = met > 0 ? s_need[met - 1] : 0;
-    if (ok) {
-        const int gone = (int)given;
-        auto given_back = [&](int i) {                        // the i-th page given back
-            const int b = cb_upper(s_back, B, i), w = want_len[b];
-            return table[(size_t)b * max_pages + w / P + (w % P != 0) + i - (b > 0 ? s_back[b - 1] : 0)];
-        };
-        const int step = (int)ranks * kPageThreads;
-        for (int j = (int)rank * kPageThreads + tid; j < taken; j += step) {
-            const int b = cb_upper(s_need, B, j), w = want_len[b];
-            const int page = j < gone ? given_back(j) : stack[free0 - 1 - (j - gone)];
-            table[(size_t)b * max_pages + w / P + (w % P != 0) - (s_need[b] - j)] = page;
-        }
-        for (int i = taken + (int)rank * kPageThreads + tid; i < gone; i += step) stack[there - 1 - i] = given_back(i);
+    // (the barrier behind the sums lies behind every thread's reads of held and n_free)
+    const bool many = gridDim.x > 1;
+    if (many && tid == 0) {
+        __threadfence();
+        s_last = atomicAdd(ticket, 1u) == gridDim.x - 1u;
     }
-    // every CTA has read held and n_free
-    __syncthreads();
-    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-    if (rank != 0) return;
+    const uint32_t gone = s_back[B - 1], there = (uint32_t)free0 + gone;
+    const bool ok = stack_ok && there <= (uint32_t)num_pages;
+    // needs that are met: up to the largest sum that does not exceed what is there
+    const int met = ok ? cb_upper(s_need, B, there) : 0;
+    const uint32_t taken = met > 0 ? s_need[met - 1] : 0u;
+    if (ok) {
+        auto given_back = [&](uint32_t i) {                   // the i-th page given back
+            const int b = cb_upper(s_back, B, i);
+            return table[(size_t)b * max_pages + pages_of(want_len[b]) + (int)(i - (b > 0 ? s_back[b - 1] : 0u))];
+        };
+        const uint32_t step = gridDim.x * kPageThreads;
+        for (uint32_t j = blockIdx.x * kPageThreads + tid; j < taken; j += step) {
+            const int b = cb_upper(s_need, B, j);
+            const int page = j < gone ? given_back(j) : stack[there - 1u - j];
+            table[(size_t)b * max_pages + pages_of(want_len[b]) - (int)(s_need[b] - j)] = page;
+        }
+        for (uint32_t i = taken + blockIdx.x * kPageThreads + tid; i < gone; i += step) stack[there - 1u - i] = given_back(i);
+    }
+    if (many) {
+        __syncthreads();
+        if (!s_last) return;
+        if (tid == 0) *ticket = 0u;
+    }
     if (ok)
         for (int b = tid; b < B; b += kPageThreads) {
             int why = 0;
@@ -71,7 +79,7 @@ __global__ void __launch_bounds__(kPageThreads) cb_pages_assign_kernel(int B, in
             else if (t >= 0 && t != h) held[b] = t;
         }
     if (!ok) error = CB_ERR_INVALID_ARG;
-    else if (tid == 0) n_free[0] = (int)there - taken;
+    else if (tid == 0) n_free[0] = (int)(there - taken);
     if (error) atomicCAS(status, 0u, (uint32_t)error);
 }
 
@@ -131,13 +139,13 @@ extern "C" cb_status cb_pages_assign(cb_ctx* ctx, const int32_t* want_len, int32
                                      int32_t num_pages, int32_t* n_free, void* stream) {
     CB_CHECK_ARG(ctx && want_len && block_table && held && free_pages && n_free && max_pages >= 1 && num_pages >= 1);
     const cb_config& c = ctx->cfg;
-    if (c.batch > CB_MAX_ASSIGN) return CB_ERR_UNSUPPORTED;
+    if (c.batch > CB_MAX_ASSIGN || num_pages > (int)CB_SUM_CAP) return CB_ERR_UNSUPPORTED;
     const size_t smem = (size_t)c.batch * 8;
     if (smem > 40 * 1024) CB_CUDA(cudaFuncSetAttribute(cb_pages_assign_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, CB_MAX_ASSIGN * 8));
-    // Eight CTAs where a call may have many moves (how many is known on the device only).
-    const unsigned ctas = (long long)c.batch * max_pages > 8192 ? 8 : 1;
-    CB_CUDA(cb_launch_clusters(cb_pages_assign_kernel, ctas, ctas, kPageThreads, smem, (cudaStream_t)stream, (int)c.batch, (int)c.page_size, (int)max_pages,
-                               (int)num_pages, want_len, block_table, held, free_pages, n_free, ctx->d_status));
+    const long long entries = (long long)c.batch * max_pages;
+    const unsigned ctas = entries <= 65536 ? 1u : (unsigned)std::min<long long>(entries / 2048, ctx->num_sms);
+    CB_CUDA(cb_launch_pdl(cb_pages_assign_kernel, dim3(ctas), dim3(kPageThreads), smem, (cudaStream_t)stream, (int)c.batch, (int)c.page_size, (int)max_pages,
+                          (int)num_pages, want_len, block_table, held, free_pages, n_free, ctx->d_ticket, ctx->d_status));
     cb_count_launch(1);
     return CB_OK;
 }

@@ -28,18 +28,19 @@ struct SummaryParams {
 };
 
 // A bf16, the upper half of a word, as a double 2^-896 times as large: sign, exponent and mantissa moved to their places, which does for zero and
-// the smallest numbers too (infinity and NaN become numbers and are looked for apart).  A conversion has a quarter of these operations' rate, and the
-// kernel would wait for it.
+// the smallest numbers too (infinity and NaN become numbers and are looked for apart).
 __device__ __forceinline__ double small_double(uint32_t upper) { return __hiloint2double(((int)upper >> 3) & 0x8FFFE000, 0); }
 constexpr double kSmallDouble = 0x1p896;
 
 template <int D, int S>
-__global__ void __launch_bounds__(kSumThreads) cb_block_summary_kernel(const SummaryParams p) {
-    constexpr int HG = 256 / D, LH = D / 8, T = S / 8;        // heads of a CTA, lanes of a head, tokens of a warp
+__global__ void __launch_bounds__(kSumThreads, S == 128 ? 2 : 3) cb_block_summary_kernel(const SummaryParams p) {
+    constexpr int HG = 256 / D, LH = D / 8, WH = D / 32, T = S / 8;   // heads of a CTA, lanes of a head that load, its warps that finish it, tokens of a warp
+    constexpr int ROW = 34;                                   // channel lane * 8 + e lies at e * ROW + lane: no bank twice, written or read
     extern __shared__ uint32_t s_sums[];                      // [B]
     __shared__ uint32_t s_scratch[kSumThreads / 32];
-    __shared__ double s_part[8][256];                         // a warp's sums: channel lane * 8 + e at e * 32 + lane
-    __shared__ unsigned long long s_top[8][HG];
+    __shared__ double s_part[8][8 * ROW];                     // the warps' sums
+    __shared__ uint32_t s_bad[8];                             // of a warp's tokens: heads with a number that is not finite
+    __shared__ uint2 s_top[8];
     __shared__ __align__(16) int8_t s_out[256];
     CB_PDL_ENTRY();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -52,72 +53,104 @@ __global__ void __launch_bounds__(kSumThreads) cb_block_summary_kernel(const Sum
         else *blocks = (uint32_t)((hi - 1) / S - lo / S + 1);
     });
     if (error && blockIdx.x == 0) atomicCAS(p.status, 0u, (uint32_t)error);
-    const int groups = (p.Hkv + HG - 1) / HG;
-    const long long items = (long long)s_sums[p.B - 1] * groups;
-    for (long long item = blockIdx.x; item < items; item += gridDim.x) {
-        const uint32_t at = (uint32_t)(item / groups);
-        const int h0 = (int)(item - (long long)at * groups) * HG;
-        const int b = cb_upper(s_sums, p.B, at);
-        const int blk = p.from[b] / S + (int)(at - (b > 0 ? s_sums[b - 1] : 0u));
-        const int n = min(S, p.to[b] - blk * S);
-        const int32_t* pages = p.table + (size_t)b * p.max_pages + blk * (S / 16);
-        const int page = lane < (n + 15) / 16 ? pages[lane] : 0;
-        const bool good = __all_sync(CB_FULL, page >= 0 && page < p.num_pages);
-        const int head = h0 + lane / LH;
+    // Items: a block's 256 channels from head h0 on, all groups of heads of one block after the other, dealt to the CTAs in turn.
+    const uint32_t blocks = s_sums[p.B - 1], groups = (uint32_t)(p.Hkv + HG - 1) / HG, step_at = gridDim.x / groups, step_group = gridDim.x % groups;
+    struct Place { uint32_t at, group; };
+    auto after = [&](Place x) {
+        x.at += step_at; x.group += step_group;
+        if (x.group >= groups) { x.group -= groups; ++x.at; }
+        return x;
+    };
+    struct Item { int h0, n, page; };                         // lane l has its l-th page; n: tokens, 0 if there is no such item
+    auto locate = [&](Place x) {
+        Item i = {0, 0, 0};
+        if (x.at >= blocks) return i;
+        i.h0 = (int)x.group * HG;
+        const int b = cb_upper(s_sums, p.B, x.at);
+        const int blk = p.from[b] / S + (int)(x.at - (b > 0 ? s_sums[b - 1] : 0u));
+        i.n = min(S, p.to[b] - blk * S);
+        if (lane < (i.n + 15) / 16) i.page = p.table[(size_t)b * p.max_pages + blk * (S / 16) + lane];
+        return i;
+    };
+    uint4 v[T];
+    // All loads of an item at once.  False: a page outside the pool.
+    auto issue = [&](const Item& i) {
+        const bool good = __all_sync(CB_FULL, i.page >= 0 && i.page < p.num_pages);
+        const int head = i.h0 + lane / LH;
+#pragma unroll
+        for (int k = 0; k < T; ++k) {
+            const int t = warp + 8 * k;
+            const int pg = __shfl_sync(CB_FULL, i.page, t >> 4);
+            v[k] = make_uint4(0, 0, 0, 0);
+            if (good && t < i.n && head < p.Hkv) v[k] = *reinterpret_cast<const uint4*>(p.k_pool + (((size_t)pg * p.P + (t & 15)) * p.Hkv + head) * D + (lane % LH) * 8);
+        }
+        return good;
+    };
+    Place place = {blockIdx.x / groups, blockIdx.x % groups};
+    Item now = locate(place);
+    bool good = issue(now);
+    place = after(place);
+    Item next = locate(place);
+    while (now.n > 0) {
+        // A word's lower number by a conversion, its upper one by moving bits: half of the numbers to either pipe, both of which are slow (16 conversions, or 64
+        // operations at two to three a number, a cycle and SM; memory brings 12 numbers a cycle).
         double sum[8] = {};
-        uint32_t bits = 0;                                    // largest magnitudes, as bits of bf16
-        if (good) {
-            uint4 v[T];
+        __nv_bfloat162 most = __float2bfloat162_rn(0.f);      // largest magnitudes, NaN above all
 #pragma unroll
-            for (int k = 0; k < T; ++k) {
-                const int t = warp + 8 * k;
-                const int pg = __shfl_sync(CB_FULL, page, t >> 4);
-                v[k] = make_uint4(0, 0, 0, 0);
-                if (t < n && head < p.Hkv) v[k] = *reinterpret_cast<const uint4*>(p.k_pool + (((size_t)pg * p.P + (t & 15)) * p.Hkv + head) * D + (lane % LH) * 8);
-            }
+        for (int k = 0; k < T; ++k) {
+            const uint32_t w[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
 #pragma unroll
-            for (int k = 0; k < T; ++k) {
-                const uint32_t w[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    sum[2 * e] += small_double(w[e] << 16);
-                    sum[2 * e + 1] += small_double(w[e]);
-                    bits = __vmaxu2(bits, w[e] & 0x7FFF7FFFu);
-                }
+            for (int e = 0; e < 4; ++e) {
+                sum[2 * e] += (double)__uint_as_float(w[e] << 16);
+                sum[2 * e + 1] += small_double(w[e]);
+                most = __hmax2_nan(most, __habs2(reinterpret_cast<const __nv_bfloat162&>(w[e])));
             }
         }
+        // the next item's keys are on their way while this one's sums are put together
+        const Item it = now;
+        const bool it_good = good;
+        now = next;
+        good = issue(now);
+        place = after(place);
+        next = locate(place);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) s_part[warp][e * 32 + lane] = sum[e];
-        unsigned long long top = max(bits & 0xFFFFu, bits >> 16) >= 0x7F80u ? 0x7FF0000000000000ull : 0ull;
-        if (lane % LH == 0) s_top[warp][lane / LH] = 0ull;
-        __syncwarp();
-        if (top) s_top[warp][lane / LH] = top;
+        for (int e = 0; e < 8; ++e) s_part[warp][e * ROW + lane] = sum[e];
+        const uint32_t bits = reinterpret_cast<const uint32_t&>(most) & 0x7FFF7FFFu;
+        const uint32_t bad = __ballot_sync(CB_FULL, max(bits & 0xFFFFu, bits >> 16) >= 0x7F80u);
+        if (lane == 0) s_bad[warp] = bad;
         __syncthreads();
+        // a channel per thread: its mean, and the largest magnitude of its head's
         double m = 0.0;
+        uint32_t any_bad = 0;
 #pragma unroll
-        for (int w = 0; w < 8; ++w) { m += s_part[w][tid]; top = max(top, s_top[w][lane / LH]); }
-        m = __ddiv_rn(__dmul_rn(m, kSmallDouble), (double)n);
-        // the largest magnitude, as bits
-        top = max(top, (unsigned long long)__double_as_longlong(m) & 0x7FFFFFFFFFFFFFFFull);
+        for (int w = 0; w < 8; ++w) { m += s_part[w][(tid & 7) * ROW + (tid >> 3)]; any_bad |= s_bad[w]; }
+        if (tid & 1) m *= kSmallDouble;
+        m = it.n == S ? m * (1.0 / S) : __ddiv_rn(m, (double)it.n);   // (the same: S is a power of two)
+        const int group = tid / D;
+        const bool finite = (any_bad >> (group * LH) & (uint32_t)((1ull << LH) - 1ull)) == 0u;
+        const uint32_t hi = (uint32_t)__double2hiint(m) & 0x7FFFFFFFu, lo = (uint32_t)__double2loint(m);
+        const uint32_t top_hi = __reduce_max_sync(CB_FULL, hi), top_lo = __reduce_max_sync(CB_FULL, hi == top_hi ? lo : 0u);
+        if (lane == 0) s_top[warp] = make_uint2(top_hi, top_lo);
+        __syncthreads();
+        uint2 top = make_uint2(0u, 0u);
 #pragma unroll
-        for (int o = LH / 2; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(CB_FULL, top, o));
+        for (int w = 0; w < WH; ++w) {
+            const uint2 x = s_top[group * WH + w];
+            if (x.x > top.x || (x.x == top.x && x.y > top.y)) top = x;
+        }
+        const double a = __hiloint2double((int)top.x, (int)top.y);
+        // The whole number by a quotient in 32 bits, off by less than 127 * 2^-21, unless that lies near half way between two; then by the one in 64.
+        const float f = __fdividef((float)m * 127.f, (float)a), whole = rintf(f);
+        int q = (int)whole;
+        if (!(fabsf(fabsf(f - whole) - 0.5f) > 0.001f) || !(a > 1e-30 && a < 1e36)) q = __double2int_rn(__ddiv_rn(__dmul_rn(m, 127.0), fmax(a, 1e-30)));
+        s_out[tid] = finite ? (int8_t)q : (int8_t)0;
+        const int first = __shfl_sync(CB_FULL, it.page, 0);
+        if (it_good && tid % D == 0 && it.h0 + group < p.Hkv) p.scale[(size_t)first * p.Hkv + it.h0 + group] = finite ? (float)__ddiv_rn(a, 127.0) : INFINITY;
         __syncthreads();
-        if (lane % LH == 0) s_top[warp][lane / LH] = top;
-        __syncthreads();
-#pragma unroll
-        for (int w = 0; w < 8; ++w) top = max(top, s_top[w][lane / LH]);
-        const double a = __longlong_as_double((long long)top);
-        const bool finite = top < 0x7FF0000000000000ull;
-        const int q = finite ? __double2int_rn(__ddiv_rn(__dmul_rn(m, 127.0), fmax(a, 1e-30))) : 0;
-        s_out[lane * 8 + warp] = (int8_t)q;
-        const int first = __shfl_sync(CB_FULL, page, 0);
-        if (good && warp == 0 && lane % LH == 0 && head < p.Hkv)
-            p.scale[(size_t)first * p.Hkv + head] = finite ? (float)__ddiv_rn(a, 127.0) : INFINITY;
-        __syncthreads();
-        if (!good) {
+        if (!it_good) {
             if (tid == 0) atomicCAS(p.status, 0u, (uint32_t)CB_ERR_INVALID_ARG);
-        } else if (tid < 64 && h0 * D + tid * 4 < p.Hkv * D) {
-            *reinterpret_cast<uint32_t*>(p.mean + ((size_t)first * p.Hkv + h0) * D + tid * 4) = *reinterpret_cast<const uint32_t*>(s_out + tid * 4);
+        } else if (tid < 64 && it.h0 * D + tid * 4 < p.Hkv * D) {
+            *reinterpret_cast<uint32_t*>(p.mean + ((size_t)first * p.Hkv + it.h0) * D + tid * 4) = *reinterpret_cast<const uint32_t*>(s_out + tid * 4);
         }
     }
 }
@@ -284,7 +317,7 @@ extern "C" cb_status cb_block_summary(cb_ctx* ctx, const cb_block_summary_args* 
     const size_t smem = (size_t)c.batch * 4;
     const auto launch = [&](auto kernel) -> cb_status {
         if (smem > 16 * 1024) CB_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, CB_MAX_ASSIGN * 4));
-        CB_CUDA(cb_launch_pdl(kernel, dim3(ctx->num_sms * 4), dim3(kSumThreads), smem, (cudaStream_t)stream, p));
+        CB_CUDA(cb_launch_pdl(kernel, dim3(ctx->num_sms * (a->block == 128 ? 2 : 3)), dim3(kSumThreads), smem, (cudaStream_t)stream, p));
         cb_count_launch(1);
         return CB_OK;
     };

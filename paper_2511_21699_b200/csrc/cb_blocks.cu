@@ -76,13 +76,16 @@ __global__ void __launch_bounds__(kSumThreads, S == 128 ? 2 : 3) cb_block_summar
     // All loads of an item at once.  False: a page outside the pool.
     auto issue = [&](const Item& i) {
         const bool good = __all_sync(CB_FULL, i.page >= 0 && i.page < p.num_pages);
-        const int head = i.h0 + lane / LH;
+        const int head = i.h0 + lane / LH, n = good && head < p.Hkv ? i.n : 0;
+        // token warp + 8 k of the block is row warp + 8 (k & 1) of its page k / 2
+        const __nv_bfloat16* const at = p.k_pool + ((size_t)warp * p.Hkv + head) * D + (lane % LH) * 8;
+        const size_t row = (size_t)p.Hkv * D;
 #pragma unroll
-        for (int k = 0; k < T; ++k) {
-            const int t = warp + 8 * k;
-            const int pg = __shfl_sync(CB_FULL, i.page, t >> 4);
-            v[k] = make_uint4(0, 0, 0, 0);
-            if (good && t < i.n && head < p.Hkv) v[k] = *reinterpret_cast<const uint4*>(p.k_pool + (((size_t)pg * p.P + (t & 15)) * p.Hkv + head) * D + (lane % LH) * 8);
+        for (int k = 0; k < T; k += 2) {
+            const __nv_bfloat16* src = at + (size_t)__shfl_sync(CB_FULL, i.page, k >> 1) * (16 * row);
+            v[k] = v[k + 1] = make_uint4(0, 0, 0, 0);
+            if (warp + 8 * k < n) v[k] = *reinterpret_cast<const uint4*>(src);
+            if (warp + 8 * k + 8 < n) v[k + 1] = *reinterpret_cast<const uint4*>(src + 8 * row);
         }
         return good;
     };

@@ -18,16 +18,18 @@
 
 namespace {
 
-constexpr int kTokWarps = 4, kTokThreads = 32 * kTokWarps, kTokStages = 2;
-
-template <int D, int NT>
+// WARPS: 8 of two stages where all CTAs are resident at once, one an SM, and the launch is as long as its longest warp; 4 of three stages, two CTAs an SM, where there
+// are more, and one's end should lie beside the middle of another.  (Stages of 8 KB with 128 dims; twice as many with 64.  64 sequences of 8 kv heads: 83 to 86 us with 4 warps of three
+// stages, 86 of two, 90 with 8 of two; one sequence: 7.5 with 4, 6.7 with 8.)
+template <int D, int NT, int WARPS_>
 struct TokCfg {
+    static constexpr int WARPS = WARPS_, THREADS = 32 * WARPS, STAGES = (WARPS == 8 ? 2 : 3) * (128 / D);
     static constexpr uint32_t PAGE = 16 * D * 2;              // a page's keys, or values, of one head
-    static constexpr uint32_t WARP = kTokStages * 2 * PAGE;
+    static constexpr uint32_t WARP = STAGES * 2 * PAGE;
     static constexpr int ROWS = 8 * NT, STRIDE = D + 4;       // of a part's output in floats: eight columns of four queries meet no bank twice
     static constexpr uint32_t PART = ROWS * STRIDE * 4;       // fits the warp's ring
-    static constexpr uint32_t OFF_BAR = kTokWarps * WARP, OFF_ML = OFF_BAR + kTokWarps * kTokStages * 8 + 16;   // [warps][rows] maximum, sum; abort flag before it
-    static constexpr uint32_t OFF_GATHER = OFF_ML + kTokWarps * ROWS * 8;                                        // [cluster][rows][STRIDE], maximum and sum in the last places
+    static constexpr uint32_t OFF_BAR = WARPS * WARP, OFF_ML = OFF_BAR + (WARPS * STAGES * 8 + 15) / 16 * 16 + 16;   // [warps][rows] maximum, sum; abort flag before it
+    static constexpr uint32_t OFF_GATHER = OFF_ML + WARPS * ROWS * 8;                                        // [cluster][rows][STRIDE], maximum and sum in the last places
     static_assert(PART <= WARP, "a warp's part lies in its ring");
 };
 
@@ -49,9 +51,9 @@ __device__ __forceinline__ void mma_bf16(float* c, const uint32_t* a, uint32_t b
 
 struct TokMaps { CUtensorMap k, v; };
 
-template <int D, int NT>
-__global__ void __launch_bounds__(kTokThreads) cb_block_token_kernel(const CbListParams p, const __grid_constant__ TokMaps maps) {
-    using C = TokCfg<D, NT>;
+template <int D, int NT, int WARPS>
+__global__ void __launch_bounds__(32 * WARPS) cb_block_token_kernel(const CbListParams p, const __grid_constant__ TokMaps maps) {
+    using C = TokCfg<D, NT, WARPS>;
     extern __shared__ __align__(1024) uint8_t tok_smem[];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, gid = lane >> 2, tig = lane & 3;
     const uint32_t sbase = smem_u32(tok_smem);
@@ -59,7 +61,7 @@ __global__ void __launch_bounds__(kTokThreads) cb_block_token_kernel(const CbLis
         if (tid == 0) atomicCAS(p.status, 0u, (uint32_t)CB_ERR_UNSUPPORTED);
         return;
     }
-    const uint32_t ring = sbase + warp * C::WARP, bars = sbase + C::OFF_BAR + warp * kTokStages * 8;
+    const uint32_t ring = sbase + warp * C::WARP, bars = sbase + C::OFF_BAR + warp * C::STAGES * 8;
     volatile int* const s_abort = reinterpret_cast<volatile int*>(tok_smem + C::OFF_ML - 16);
     float2* const s_ml = reinterpret_cast<float2*>(tok_smem + C::OFF_ML);
     float* const s_gather = reinterpret_cast<float*>(tok_smem + C::OFF_GATHER);
@@ -67,7 +69,7 @@ __global__ void __launch_bounds__(kTokThreads) cb_block_token_kernel(const CbLis
     asm("mov.u32 %0, %cluster_ctarank;" : "=r"(rank));
     asm("mov.u32 %0, %cluster_nctarank;" : "=r"(ranks));
     if (lane == 0) {
-        for (int s = 0; s < kTokStages; ++s) mbar_init(bars + 8 * s, 1);
+        for (int s = 0; s < C::STAGES; ++s) mbar_init(bars + 8 * s, 1);
         if (warp == 0) { *s_abort = 0; tma_prefetch_desc(&maps.k); tma_prefetch_desc(&maps.v); }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -82,12 +84,12 @@ __global__ void __launch_bounds__(kTokThreads) cb_block_token_kernel(const CbLis
     if (ranks > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
     const int nb = cb_blocks_of(p.ctx_len[b], p.l.shift), keys = s.ctx + s.n, all = (keys + 15) / 16;
     const int pg0 = (int)((long long)all * rank / ranks), pg1 = (int)((long long)all * (rank + 1) / ranks);
-    const int count = pg1 - pg0 > warp ? (pg1 - pg0 - warp + kTokWarps - 1) / kTokWarps : 0;   // pages pg0 + warp, + kTokWarps, ...
+    const int count = pg1 - pg0 > warp ? (pg1 - pg0 - warp + WARPS - 1) / WARPS : 0;   // pages pg0 + warp, + WARPS, ...
     // Page numbers, a lane's of 32 pages at a time, the next 32 beside them: two dependent reads each.
     auto page_of = [&](int k) {
         int page = p.num_pages;                               // out of the pool: the copy fills zeros
         if (k < count) {
-            const int col = cb_page_column(p.l, b, p.Hkv, kh, nb, pg0 + warp + k * kTokWarps);
+            const int col = cb_page_column(p.l, b, p.Hkv, kh, nb, pg0 + warp + k * WARPS);
             if ((uint32_t)col < (uint32_t)p.max_pages) page = __ldg(p.block_table + (size_t)b * p.max_pages + col);
             if ((uint32_t)page >= (uint32_t)p.num_pages) page = p.num_pages;
         }
@@ -97,14 +99,14 @@ __global__ void __launch_bounds__(kTokThreads) cb_block_token_kernel(const CbLis
     auto fetch = [&](int k) {                                 // the warp's k-th page into its stage; page_now is that of its 32 or the 32 before
         const int page = __shfl_sync(CB_FULL, k & 32 ? page_later : page_now, k & 31);
         if (lane == 0) {
-            const uint32_t st = k % kTokStages, at = ring + st * 2 * C::PAGE;
+            const uint32_t st = k % C::STAGES, at = ring + st * 2 * C::PAGE;
             mbar_expect_tx(bars + 8 * st, 2 * C::PAGE);
             tma_load_5d(at, &maps.k, bars + 8 * st, 0, 0, 0, page * 2, kh);
             tma_load_5d(at + C::PAGE, &maps.v, bars + 8 * st, 0, 0, 0, page * 2, kh);
         }
         __syncwarp();
     };
-    for (int k = 0; k < min(count, kTokStages); ++k) fetch(k);
+    for (int k = 0; k < min(count, C::STAGES); ++k) fetch(k);
     // the queries' fragments: row r of the unit (token r / G, head r % G) is column r; what does not exist is zero
     const int rows = s.n * p.G;
     uint32_t q[NT][D / 16][2];
@@ -134,9 +136,9 @@ __global__ void __launch_bounds__(kTokThreads) cb_block_token_kernel(const CbLis
     };
     bool ok = true;
     for (int k = 0; k < count; ++k) {
-        const uint32_t st = k % kTokStages, kb = ring + st * 2 * C::PAGE, vb = kb + C::PAGE;
-        if (!(ok = mbar_wait(bars + 8 * st, (k / kTokStages) & 1, s_abort, p.status))) break;
-        const int key0 = (pg0 + warp + k * kTokWarps) * 16;
+        const uint32_t st = k % C::STAGES, kb = ring + st * 2 * C::PAGE, vb = kb + C::PAGE;
+        if (!(ok = mbar_wait(bars + 8 * st, (k / C::STAGES) & 1, s_abort, p.status))) break;
+        const int key0 = (pg0 + warp + k * WARPS) * 16;
         float sc[NT][4] = {};
 #pragma unroll
         for (int d = 0; d < D / 16; ++d) {
@@ -195,7 +197,7 @@ __global__ void __launch_bounds__(kTokThreads) cb_block_token_kernel(const CbLis
             for (int t = 0; t < NT; ++t) mma_bf16(o[t][d], a, pb[t][0], pb[t][1]);
         }
         __syncwarp();                                         // the stage has been read
-        const int next = k + kTokStages;
+        const int next = k + C::STAGES;
         if ((next & 31) == 0 && next > 0) {                   // on to the next 32 page numbers: the half that they are not in is free
             if (next & 32) page_now = page_of(next + 32 + lane);
             else page_later = page_of(next + 32 + lane);
@@ -232,16 +234,16 @@ __global__ void __launch_bounds__(kTokThreads) cb_block_token_kernel(const CbLis
         if (c == 0 && p.lse) p.lse[at] = (mx + log2f(sum)) * 0.6931471805599453f;
     };
     const uint32_t gather0 = ranks > 1 ? cluster_addr(smem_u32(s_gather), 0) + rank * (uint32_t)(C::ROWS * C::STRIDE * 4) : 0u;
-    for (int x = tid; x < QUADS; x += kTokThreads) {
+    for (int x = tid; x < QUADS; x += C::THREADS) {
         const int r = x / (D / 4), c = x % (D / 4) * 4;
         if (r >= rows) break;
         float mx = -INFINITY, sum = 0.f;
-        float2 ml[kTokWarps];
+        float2 ml[WARPS];
 #pragma unroll
-        for (int w = 0; w < kTokWarps; ++w) { ml[w] = s_ml[w * C::ROWS + r]; mx = fmaxf(mx, ml[w].x); }
+        for (int w = 0; w < WARPS; ++w) { ml[w] = s_ml[w * C::ROWS + r]; mx = fmaxf(mx, ml[w].x); }
         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-        for (int w = 0; w < kTokWarps; ++w) {
+        for (int w = 0; w < WARPS; ++w) {
             const float f = ml[w].x == -INFINITY ? 0.f : ex2(ml[w].x - mx);
             const float4 y = *reinterpret_cast<const float4*>(tok_smem + w * C::WARP + (r * C::STRIDE + c) * 4);
             sum = fmaf(f, ml[w].y, sum);
@@ -258,7 +260,7 @@ __global__ void __launch_bounds__(kTokThreads) cb_block_token_kernel(const CbLis
         __syncwarp();
         asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
         if (rank == 0)
-            for (int x = tid; x < QUADS; x += kTokThreads) {
+            for (int x = tid; x < QUADS; x += C::THREADS) {
                 const int r = x / (D / 4), c = x % (D / 4) * 4;
                 if (r >= rows) break;
                 float mx = -INFINITY, sum = 0.f;
@@ -278,9 +280,9 @@ __global__ void __launch_bounds__(kTokThreads) cb_block_token_kernel(const CbLis
         for (int k = 0; k < 64; ++k) __nanosleep(1000);
 }
 
-template <int D, int NT>
+template <int D, int NT, int WARPS>
 cb_status launch_token(const cb_ctx* ctx, const CbListParams& p, int ctas, cudaStream_t st) {
-    using C = TokCfg<D, NT>;
+    using C = TokCfg<D, NT, WARPS>;
     static std::mutex mutex;
     static size_t have[kMaxDevices];
     const size_t smem = C::OFF_GATHER + (ctas > 1 ? (size_t)ctas * C::ROWS * C::STRIDE * 4 : 0);
@@ -289,11 +291,15 @@ cb_status launch_token(const cb_ctx* ctx, const CbListParams& p, int ctas, cudaS
     {
         std::lock_guard<std::mutex> lock(mutex);
         size_t fresh = 0;
-        CB_CUDA(cb_allow_smem(cb_block_token_kernel<D, NT>, smem, ctx->device >= 0 && ctx->device < kMaxDevices ? &have[ctx->device] : &fresh));
+        CB_CUDA(cb_allow_smem(cb_block_token_kernel<D, NT, WARPS>, smem, ctx->device >= 0 && ctx->device < kMaxDevices ? &have[ctx->device] : &fresh));
     }
-    CB_CUDA(cb_launch_clusters(cb_block_token_kernel<D, NT>, (unsigned)((long long)p.B * p.Hkv * ctas), (unsigned)ctas, kTokThreads, smem, st, p, maps));
+    CB_CUDA(cb_launch_clusters(cb_block_token_kernel<D, NT, WARPS>, (unsigned)((long long)p.B * p.Hkv * ctas), (unsigned)ctas, C::THREADS, smem, st, p, maps));
     cb_count_launch(1);
     return CB_OK;
+}
+template <int D, int NT>
+cb_status launch_warps(const cb_ctx* ctx, const CbListParams& p, bool resident, int ctas, cudaStream_t st) {
+    return resident ? launch_token<D, NT, 8>(ctx, p, ctas, st) : launch_token<D, NT, 4>(ctx, p, ctas, st);
 }
 
 }  // namespace
@@ -303,10 +309,12 @@ cb_status cb_block_launch_token(cb_ctx* ctx, const CbListParams& given, cudaStre
     if (p.P != 16 || p.num_pages >= 1 << 29) return CB_ERR_UNSUPPORTED;   // (a page's coordinate is twice its number)
     p.g_inv = 65536u / (uint32_t)p.G + 1u;                    // x / G = x * g_inv >> 16 for x < 256
     const long long units = (long long)p.B * p.Hkv, pages = (std::min<long long>(p.max_keys, ((long long)p.l.n_select << p.l.shift) + p.max_chunk) + 15) / 16;
-    // A cluster shares a unit where there are few, or to even out the last wave, as long as a warp has two pages.
+    // A cluster shares a unit while all CTAs find an SM of their own and four pages each (8 sequences of 8 kv heads, 2,048 keys: 11.1 us with 128 CTAs, 14.3 with 64, 28 with
+    // 512; 8 kv heads of one sequence, 512 keys: 5.1 us with 64 CTAs, 6.0 with 32).
+    const bool resident = units <= ctx->num_sms;
     int ctas = 1;
-    while (ctas < 8 && units * ctas < 4ll * ctx->num_sms && pages >= ctas * 2 * 2 * kTokWarps) ctas *= 2;
+    while (ctas < 8 && units * ctas * 2 <= ctx->num_sms && pages >= ctas * 2 * 4) ctas *= 2;
     const bool few = p.max_chunk * p.G <= 8;
-    if (p.D == 128) return few ? launch_token<128, 1>(ctx, p, ctas, st) : launch_token<128, 2>(ctx, p, ctas, st);
-    return few ? launch_token<64, 1>(ctx, p, ctas, st) : launch_token<64, 2>(ctx, p, ctas, st);
+    if (p.D == 128) return few ? launch_warps<128, 1>(ctx, p, resident, ctas, st) : launch_warps<128, 2>(ctx, p, resident, ctas, st);
+    return few ? launch_warps<64, 1>(ctx, p, resident, ctas, st) : launch_warps<64, 2>(ctx, p, resident, ctas, st);
 }

@@ -495,9 +495,9 @@ cb_status cb_slot_map(cb_ctx* ctx, const cb_slot_map_args* args, void* stream);
  * summary (its mean key, in 8 bits), and per sequence and kv head the queries of a chunk or of a tree choose n_select blocks by it.
  *
  * cb_block_summary: the summaries of the blocks that new tokens touch, after their keys are in the pages (cb_chunk_append, cb_kv_commit).  For
- * every block that holds one of the positions from_len[b] .. to_len[b] - 1 of sequence b, over its tokens below to_len[b], m the mean of a head's keys:
+ * every block that holds one of the positions from_len[b] .. to_len[b] - 1 of sequence b, over its tokens below to_len[b], m = sum of a head's keys / tokens:
  *   k_scale = max |m| / 127,   k_mean[d] = m[d] * 127 / max |m| rounded to the nearest whole number (half way: to the even one)
- * in 64 bits, and so independent of any order of addition.  They are stored with the block's first page.
+ * each operation in 64 bits, where the sum is exact, and so independent of any order of addition.  They are stored with the block's first page.
  *   k_pool   bf16 [num_pages, P, Hkv, D];  block_table int32 [batch, max_pages];  from_len, to_len int32 [batch]
  *   k_mean   int8 [num_pages, Hkv, D], k_scale float [num_pages, Hkv]     other pages' rows are left as they were
  * A head whose mean is not finite gets k_scale = +inf and zeros, which cb_block_select puts before all others.  A sequence with

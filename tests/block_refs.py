@@ -34,8 +34,10 @@ def assign(want, table, held, free, n_free):
 
 
 def summary(keys):
-    """keys [n, heads, D] of a block's tokens: (k_mean int, k_scale), 64 bits."""
-    m = keys.to(F8).mean(0)
+    """keys [n, heads, D] of a block's tokens: (k_mean int, k_scale), 64 bits.  The mean is a quotient (a mean by multiplication with 1 / n, which has no exact form
+    for n = 5, say, puts numbers half way between two steps on the other side)."""
+    s = keys.to(F8).sum(0)
+    m = s / torch.full_like(s, keys.shape[0])
     top = m.abs().amax(-1, keepdim=True)
     return torch.round(127 * m / top.clamp(min=1e-30)).long(), (top / 127)[..., 0]
 

@@ -93,32 +93,26 @@ __global__ void __launch_bounds__(kManyThreads, 1) cb_select_many_kernel(const C
             }
         };
         if (worker && own > 0) load_rows(0);
-        // Largest magnitude of the queries.  Of up to 512 they stay in registers on the way to shared memory.
-        constexpr int V = kManyRows * (D / 8) / kManyWorkers; // 16-byte pieces of a thread
-        uint4 v[V];
-        auto load_queries = [&](int q0) {
-            const int n = min(kManyRows, nq - q0), padded = min((n + 31) & ~31, kManyRows);
+        // 512 queries, eight 16-byte pieces of a thread under way at a time: to find their largest magnitude, and again (from L2) to make whole numbers of them.
+        constexpr int V = kManyRows * (D / 8) / kManyWorkers, STEP = V < 8 ? V : 8;
+        auto queries = [&](int q0, auto&& use) {
+            const int n = min(kManyRows, nq - q0), padded = min((n + 31) & ~31, kManyRows);   // (filled up with the first one)
+#pragma unroll 1
+            for (int k0 = 0; k0 < V; k0 += STEP) {
+                if (k0 * kManyWorkers >= padded * (D / 8)) break;
+                uint4 v[STEP];
 #pragma unroll
-            for (int k = 0; k < V; ++k) {
-                const int x = k * kManyWorkers + tid, i = x / (D / 8);
-                if (i < padded) v[k] = *reinterpret_cast<const uint4*>(cb_select_query<D>(p, u, q0 + (i < n ? i : 0)) + x % (D / 8) * 8);
-                else v[k] = make_uint4(0, 0, 0, 0);
-            }
-        };
-        auto store_queries = [&](float r) {
+                for (int k = 0; k < STEP; ++k) {
+                    const int x = (k0 + k) * kManyWorkers + tid, i = x / (D / 8);
+                    v[k] = *reinterpret_cast<const uint4*>(cb_select_query<D>(p, u, q0 + (i < n ? i : 0)) + x % (D / 8) * 8);
+                }
 #pragma unroll
-            for (int k = 0; k < V; ++k) {
-                const int x = k * kManyWorkers + tid, c = x % (D / 8);
-                *reinterpret_cast<uint2*>(at_swizzled(s_q, x / (D / 8), c >> 1) + (c & 1) * 8) = cb_whole8(v[k], r);
+                for (int k = 0; k < STEP; ++k) use((k0 + k) * kManyWorkers + tid, v[k]);
             }
         };
         uint32_t top = 0;
         if (worker)
-            for (int q0 = (nq - 1) / kManyRows * kManyRows; q0 >= 0; q0 -= kManyRows) {
-                load_queries(q0);
-#pragma unroll
-                for (int k = 0; k < V; ++k) top = cb_max_bits(top, v[k]);
-            }
+            for (int q0 = 0; q0 < nq; q0 += kManyRows) queries(q0, [&](int, const uint4& v) { top = cb_max_bits(top, v); });
         top = __reduce_max_sync(CB_FULL, max(top & 0xFFFFu, top >> 16));
         if (lane == 0) s_scratch[warp] = top;
         for (int j = tid; j < p.key_words; j += kManyThreads) s_key[j] = 0x80000000u;
@@ -134,11 +128,12 @@ __global__ void __launch_bounds__(kManyThreads, 1) cb_select_many_kernel(const C
         bool stop = false;                                    // a wait ran out: known to all threads at once
         for (int q0 = 0; q0 < nq && !stop; q0 += kManyRows) {
             const int n = min(kManyRows, nq - q0), padded = (n + 31) & ~31, halves = (padded + 255) / 256;
-            if (q0 > 0) {
-                __syncthreads();                              // the products of the queries before have been read
-                if (worker) load_queries(q0);
-            }
-            if (worker) store_queries(r);
+            if (q0 > 0) __syncthreads();                      // the products of the queries before have been read
+            if (worker)
+                queries(q0, [&](int x, const uint4& v) {
+                    const int c = x % (D / 8);
+                    *reinterpret_cast<uint2*>(at_swizzled(s_q, x / (D / 8), c >> 1) + (c & 1) * 8) = cb_whole8(v, r);
+                });
             for (int i0 = 0; i0 < own && !stop; i0 += kManyRows) {
                 if (i0 > 0 || (q0 > 0 && own > kManyRows)) {
                     __syncthreads();
@@ -170,12 +165,20 @@ __global__ void __launch_bounds__(kManyThreads, 1) cb_select_many_kernel(const C
                         if (!(ok = mbar_wait(bar_full(mine), (job / 2) & 1, s_abort, p.status))) break;
                         tc_fence_after();
                         int best = INT32_MIN;
-                        for (int c = columns * 128; c < min(cols, columns * 128 + 128); c += 32) {
-                            uint32_t x[32];
-                            CB_TMEM_LD32(x, 0, tmem + mine * 256 + c + ((uint32_t)(quarter * 32) << 16));
+                        // (64 columns under way at once, what lies behind the last query's 32 not looked at)
+                        for (int c = columns * 128; c < min(cols, columns * 128 + 128); c += 64) {
+                            uint32_t x[32], y[32];
+                            const uint32_t at = tmem + mine * 256 + c + ((uint32_t)(quarter * 32) << 16);
+                            CB_TMEM_LD32(x, 0, at);
+                            if (c + 32 < cols) CB_TMEM_LD32(y, 0, at + 32);
                             CB_TMEM_WAIT_LD32(x);
 #pragma unroll
                             for (int k = 0; k < 32; k += 2) best = max(best, max((int)x[k], (int)x[k + 1]));
+                            if (c + 32 < cols) {
+                                CB_TMEM_WAIT_LD32(y);
+#pragma unroll
+                                for (int k = 0; k < 32; k += 2) best = max(best, max((int)y[k], (int)y[k + 1]));
+                            }
                         }
                         tc_fence_before();
                         __syncwarp();

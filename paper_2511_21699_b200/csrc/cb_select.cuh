@@ -58,21 +58,14 @@ __device__ __forceinline__ uint32_t cb_max_bits(uint32_t top, const uint4& v) {
 }
 __device__ __forceinline__ float cb_whole_factor(uint32_t top_bits) { return __fdiv_rn(127.f, fmaxf(__uint_as_float(top_bits << 16), 1e-30f)); }
 // Eight bf16 times r, rounded to whole numbers, as eight bytes.  Adding 1.5 * 2^23 rounds to a whole number and leaves it in the low bits (a conversion has
-// a quarter of that rate).
+// a quarter of that rate).  Two roundings, as the definition has them: packed mul.rn.f32x2 and add.rn.f32x2 come out as one fused operation with one.
 __device__ __forceinline__ uint2 cb_whole8(const uint4& v, float r) {
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
     uint32_t o[4];
-    uint64_t rr, magic;
-    asm("mov.b64 %0, {%1, %1};" : "=l"(rr) : "f"(r));
-    asm("mov.b64 %0, {%1, %1};" : "=l"(magic) : "f"(12582912.f));
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-        uint64_t x;
-        uint32_t lo, hi;
-        asm("mov.b64 %0, {%1, %2};" : "=l"(x) : "r"(w[e] << 16), "r"(w[e] & 0xFFFF0000u));
-        asm("mul.rn.f32x2 %0, %0, %1;" : "+l"(x) : "l"(rr));
-        asm("add.rn.f32x2 %0, %0, %1;" : "+l"(x) : "l"(magic));
-        asm("mov.b64 {%0, %1}, %2;" : "=r"(lo), "=r"(hi) : "l"(x));
+        const uint32_t lo = __float_as_uint(__fadd_rn(__fmul_rn(__uint_as_float(w[e] << 16), r), 12582912.f));
+        const uint32_t hi = __float_as_uint(__fadd_rn(__fmul_rn(__uint_as_float(w[e] & 0xFFFF0000u), r), 12582912.f));
         o[e] = __byte_perm(lo, hi, 0x0040);
     }
     return make_uint2(__byte_perm(o[0], o[1], 0x5410), __byte_perm(o[2], o[3], 0x5410));

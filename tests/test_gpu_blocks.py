@@ -263,3 +263,23 @@ def test_selection_of_no_rows_at_all():
     s = Scored([6400, 100], 2, 64, 64)
     out, st = _select(s, torch.empty(0, 4, 64, device="cuda", dtype=BF), 5, q_start=np.zeros(3, int))
     assert st == OK and (out == -1).all()
+
+
+@pytest.mark.parametrize("n", [1, 9])
+def test_many_rows_of_many_blocks(n):
+    """Enough choices that a query rounded the other way anywhere, or a score off by one, changes some of them: 512 lists of 32 out of 512 blocks, by 4 queries (in registers) and
+    by 36 (through shared memory)."""
+    s = Scored([32768 - 17 * b for b in range(64)], 8, 128, 64, seed=n)
+    start, q = _chunks([n] * 64, 32, 128, s.c.g)
+    out, st = _select(s, q, 32, q_start=start, hints=True)
+    assert st == OK
+    rows = q.view(64, n, 8, 4, 128).permute(0, 2, 1, 3, 4).reshape(64, 8, n * 4, 128).float()
+    top = rows.abs().amax((2, 3), keepdim=True)
+    eighth = torch.round(rows * (torch.full_like(top, 127.0) / top)).to(F8)
+    for b in range(64):
+        at = s.first_pages(b)
+        dot = torch.matmul(eighth[b], s.mean[at].to(F8).permute(1, 2, 0)).amax(1)            # [heads, blocks]
+        score = dot.float() * s.scale[at].t()
+        score[:, 0] = score[:, -2:] = math.inf
+        best = torch.sort(score, dim=1, descending=True, stable=True)[1][:, :32].sort(1)[0]
+        assert out[b].tolist() == best.tolist(), b

@@ -1,7 +1,8 @@
 // Attention over selected blocks for few rows a unit: single tokens, up to 16 rows x heads of a kv head's group.
 //
 // Such a unit is a stream: two flops a byte and row.  (A tcgen05 tile has 128 rows, of which a token fills 1 to 16; chunk attention's kernel takes such units too, with
-// a schedule, a ring and an epilogue made for tiles, 13.9 us for one token and 110 for 64 with lists of 2,048 tokens.)  So here a warp works for itself: it has a ring of its own that an
+// a schedule, a ring and an epilogue made for tiles: 13.9 us for one token and 110 for 64 with lists of 2,048 tokens, 8 kv heads of 128, where this one takes 6.6 and 84, 95% of the copy
+// rate.)  So here a warp works for itself: it has a ring of its own that an
 // asynchronous copy fills with a page of keys and values at a time, m16n8k16 products with the keys (then the values' columns) as the 16 rows and the queries as
 // the 8 columns, and its own running softmax.  Nobody waits for anybody until the end, where the block's warps, and a cluster's blocks through distributed shared
 // memory, put their parts together.
@@ -90,7 +91,7 @@ __global__ void __launch_bounds__(32 * WARPS) cb_block_token_kernel(const CbList
         int page = p.num_pages;                               // out of the pool: the copy fills zeros
         if (k < count) {
             const int col = cb_page_column(p.l, b, p.Hkv, kh, nb, pg0 + warp + k * WARPS);
-            if ((uint32_t)col < (uint32_t)p.max_pages) page = __ldg(p.block_table + (size_t)b * p.max_pages + col);
+            if ((uint32_t)col < (uint32_t)p.max_pages) page = p.block_table[(size_t)b * p.max_pages + col];
             if ((uint32_t)page >= (uint32_t)p.num_pages) page = p.num_pages;
         }
         return page;

@@ -19,6 +19,8 @@
 // of keys and values: 188 to 207 us, 5.3 to 5.8 TB/s.  One token over 4 k, 32 heads: 23.8 us, nearly all of it before the first tile and behind the last.
 // Of the spills (124 to 132 bytes a thread) three to four loads and one store a tile and softmax warp lie in the tile loop, beside some 450 instructions; the others
 // are a unit's, some ten (counted over prompts of 1 k to 4 k).
+//
+// The kernel is a template of what it is given: all of the context (cb_chunk_tc.cu), or selected blocks of it, for chunks or for the nodes of trees (cb_block_tc.cu).
 #pragma once
 #include <cuda.h>
 
@@ -423,7 +425,7 @@ __global__ void __launch_bounds__(kThreads, 1) cb_chunk_tc_kernel(const P p, con
             const int token = first + token_of(row);
             const bool row_valid = row < RT && token < u->n;
             const bool warp_active = (wq * 32) < RT && first + token_of(wq * 32) < u->n;   // row 0 of the warp is valid
-            const int limit = TREE ? u->ctx : u->ctx + token + 1;   // keys that this row sees (of the context)
+            const int limit = TREE ? 0 : u->ctx + token + 1;  // keys that this row sees (a tree's: all of the context)
             const uint32_t tm_O = tmem + C::O_COL + l * D + lane_addr;
             // the tile in whose last page there are slots behind the sequence's last token, for the warp that clears them
             const int unclean = u->dirty && hf == 0 && wq == 0 && (u->nrt != 2 || l == u->skip) ? u->tiles - (TREE ? 2 : 1) : -1;
@@ -454,12 +456,11 @@ __global__ void __launch_bounds__(kThreads, 1) cb_chunk_tc_kernel(const P p, con
                         if constexpr (TREE) return row_valid && k < p.W ? p.mask[(size_t)(u->row0 + token) * p.W + k] & below(u->n - 32 * k) : 0u;
                         else return 0u;
                     };
-                    const bool own_keys = TREE && i == u->tiles - 1;
                     if (!all_vis) {
-                        if (own_keys) {
+                        if (TREE && i == u->tiles - 1) {
                             vm[0] = tree_word(2 * hf); vm[1] = tree_word(2 * hf + 1); vref = tree_word(0);
                         } else {
-                            const int kv = row_valid ? limit - i * CB_KT : 0;
+                            const int kv = row_valid ? (TREE ? u->ctx : limit) - i * CB_KT : 0;
                             vm[0] = below(kv - 64 * hf); vm[1] = below(kv - 64 * hf - 32); vref = below(kv);
                         }
                     }
@@ -527,14 +528,14 @@ __global__ void __launch_bounds__(kThreads, 1) cb_chunk_tc_kernel(const P p, con
                     float lt = make_p(m_used == -INFINITY ? 0.f : m_used);
                     if (pair_sync(row_valid && !(lt <= kRowSumLimit), 0)) {          // rows that do not exist hold anything: they never ask
                         // pass 1: the row's maximum over all its visible scores (both threads of the row take it)
-                        const int kv = all_vis ? CB_KT : (row_valid ? limit - i * CB_KT : 0);
+                        const int kv = all_vis ? CB_KT : (row_valid ? (TREE ? u->ctx : limit) - i * CB_KT : 0);
                         float mx = -INFINITY;
 #pragma unroll 1
                         for (int c = 0; c < 4; ++c) {
                             uint32_t rf[32];
                             CB_TMEM_LD32(rf, 0, ts + 32 * c);
                             CB_TMEM_WAIT_LD32(rf);
-                            const uint32_t va = own_keys ? tree_word(c) : below(kv - 32 * c);
+                            const uint32_t va = TREE && i == u->tiles - 1 ? tree_word(c) : below(kv - 32 * c);
 #pragma unroll
                             for (int jx = 0; jx < 32; ++jx) mx = fmaxf(mx, ((va >> jx) & 1u) ? __uint_as_float(rf[jx]) : -INFINITY);
                         }

@@ -8,7 +8,7 @@
 //
 // cb_block_select.  A CTA, or a cluster of up to eight where there are few, per (sequence, kv head).  The queries become whole numbers of a common scale, the
 // summaries are whole numbers already, so that the scores are exact and the choice is the same however the work is cut.  64 single tokens over 1 k to 32 k tokens in blocks of
-// 64, 8 kv heads: 12.8 us, of which the longest unit's chain (lengths and pages, summaries, scores, search) is 15 k cycles; the 19 MB take 2.8.
+// 64, 8 kv heads: 11.4 us, most of it the longest unit's chain (lengths and pages, summaries, scores, search); the 19 MB take 2.8.
 #include <algorithm>
 #include <mutex>
 
@@ -161,7 +161,10 @@ __global__ void __launch_bounds__(kSumThreads, S == 128 ? 2 : 3) cb_block_summar
 }
 
 // ------------------------------------------------------------------------------------------------ selection by few queries
-constexpr int kFewThreads = 256;                              // 32 blocks a warp at a time
+// A warp takes 16 blocks at a time and has three such steps under way.  Four CTAs an SM, so that 592 units are resident at once (with 32 blocks in two steps, three
+// CTAs an SM, 68 of 512 units came in a second wave).
+constexpr int kFewThreads = 256, kFewRows = 16, kFewStages = 3, kFewStep = kFewThreads / 32 * kFewRows;
+template <int D> constexpr int kFewWarpBytes = kFewStages * kFewRows * (D + 4);   // summaries and scales
 
 __device__ __forceinline__ void mma_s8(int* c, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
@@ -175,50 +178,63 @@ __device__ __forceinline__ void mma_s8(int* c, uint32_t a0, uint32_t a1, uint32_
 // pipe is 2% busy).  A dot product does not mind the order of its terms, so the k-th step takes, of the 16-byte pieces that lane t of a row's four lanes holds
 // (piece t, and with 128 dims piece t + 4), the words that make a fragment: both sides come from memory in 16-byte pieces and go into the products as they are.
 template <int D, int NT>
-__global__ void __launch_bounds__(kFewThreads, 3) cb_select_few_kernel(const CbSelectParams p) {
+__global__ void __launch_bounds__(kFewThreads, 4) cb_select_few_kernel(const CbSelectParams p) {
     constexpr int W = D / 16, L = D / 16;                     // words of a row that a lane holds; lanes that copy a row
     extern __shared__ __align__(16) uint32_t s_dyn[];
     __shared__ __align__(16) uint32_t s_scratch[cb_pick_words<kFewThreads>];
     uint32_t* const s_key = s_dyn;
     CB_PDL_ENTRY();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, gid = lane >> 2, tig = lane & 3;
-    uint8_t* const s_rows = reinterpret_cast<uint8_t*>(s_dyn + p.key_words) + warp * (2 * 32 * D);
+    uint8_t* const s_rows = reinterpret_cast<uint8_t*>(s_dyn + p.key_words) + warp * kFewWarpBytes<D>;
+    float* const s_scale = reinterpret_cast<float*>(s_rows + kFewStages * kFewRows * D);
     uint32_t rank, ranks;
     asm("mov.u32 %0, %cluster_ctarank;" : "=r"(rank));
     asm("mov.u32 %0, %cluster_nctarank;" : "=r"(ranks));
     const int unit = blockIdx.x / ranks;
-    const int step = (int)ranks * kFewThreads, start = (int)rank * kFewThreads + warp * 32;
-    // A lane's block of the warp's 32: its first page.  Asked for beside the lengths, as far as the table has columns; a block behind the context is not used.
+    const int step = (int)ranks * kFewStep, start = (int)rank * kFewStep + warp * kFewRows;
+    // A block's first page; lanes l and l + 16 have block l of the warp's 16.  Asked for beside the lengths, as far as the table has columns; a block behind the context
+    // is not used.
+    const int32_t* const table = p.table + (size_t)(unit / p.Hkv) * p.max_pages;
     auto page_of = [&](int base) {
-        const long long col = (long long)(base + lane) << (p.shift - 4);
-        return col < p.max_pages ? p.table[(size_t)(unit / p.Hkv) * p.max_pages + col] : -1;
+        const long long col = (long long)(base + (lane & 15)) << (p.shift - 4);
+        return col < p.max_pages ? table[col] : -1;
     };
-    int page = page_of(start), page_next = page_of(start + step);
+    int pages[kFewStages];
+#pragma unroll
+    for (int k = 0; k < kFewStages; ++k) pages[k] = page_of(start + k * step);
+    int page_next = page_of(start + kFewStages * step);
     const CbSelectUnit u = cb_select_unit(p, unit, rank == 0, tid, kFewThreads);
     const int nb = u.nb, nq = u.n * p.G;
     if (nb == 0) return;
     for (int k = tid; k < cb_pick_words<kFewThreads>; k += kFewThreads) s_scratch[k] = 0u;
     if (ranks > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
     // Row i's piece c lies at piece c ^ (i & 1) * 4 (128 dims), so that eight lanes that read two rows meet no bank twice.
-    auto piece = [&](int half, int i, int c) { return s_rows + half * (32 * D) + i * D + ((D == 128 ? c ^ ((i & 1) << 2) : c) << 4); };
-    // The 32 blocks from base on into one half of the warp's rows; the next 32 are on their way while these are scored.
-    float scale = 0.f, scale_next = 0.f;
-    bool good = true, good_next = true;
-    auto load_rows = [&](int base, int half) {
-        good_next = base + lane >= nb || (page >= 0 && page < p.num_pages);
-        const int at = good_next && base + lane < nb ? page : 0;
+    auto piece = [&](int stage, int i, int c) { return s_rows + (stage * kFewRows + i) * D + ((D == 128 ? c ^ ((i & 1) << 2) : c) << 4); };
+    // The 16 blocks from base on into a stage; a page outside the pool has the scale 0.
+    auto load_rows = [&](int base, int stage, int page) {
+        if (base < nb) {
+            const int j = base + (lane & 15);
+            const bool good = j < nb && page >= 0 && page < p.num_pages;
+            const int at = good ? page : 0;
 #pragma unroll
-        for (int k = 0; k < L; ++k) {
-            const int row = k * (32 / L) + lane / L, pg = __shfl_sync(CB_FULL, at, row);
-            const int8_t* src = p.mean + ((size_t)pg * p.Hkv + u.kh) * D + lane % L * 16;
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(piece(half, row, lane % L))), "l"(src) : "memory");
+            for (int k = 0; k < kFewRows * L / 32; ++k) {
+                const int row = k * (32 / L) + lane / L, pg = __shfl_sync(CB_FULL, at, row);
+                const int8_t* src = p.mean + ((size_t)pg * p.Hkv + u.kh) * D + lane % L * 16;
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(piece(stage, row, lane % L))), "l"(src) : "memory");
+            }
+            if (lane < 16) {
+                float* const to = s_scale + stage * kFewRows + lane;
+                if (good) asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(p.scale + (size_t)at * p.Hkv + u.kh) : "memory");
+                else {
+                    *to = 0.f;
+                    if (j < nb) atomicCAS(p.status, 0u, (uint32_t)CB_ERR_INVALID_ARG);
+                }
+            }
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
-        scale_next = good_next ? p.scale[(size_t)at * p.Hkv + u.kh] : 0.f;
-        page = page_next;
-        if (base + 2 * step < nb) page_next = page_of(base + 2 * step);
     };
-    if (start < nb) load_rows(start, 0);
+#pragma unroll
+    for (int k = 0; k < kFewStages; ++k) load_rows(start + k * step, k, pages[k]);
     // the queries: each one's pieces tig and tig + 4, whole numbers of a common scale; what there is less than 8 is filled up with the first
     uint32_t w[NT][W], top = 0;
     {
@@ -245,54 +261,50 @@ __global__ void __launch_bounds__(kFewThreads, 3) cb_select_few_kernel(const CbS
         key0 = cb_cluster_first(s_key);
         cb_cluster_wait();
     }
-    int half = 0;
-    for (int base = start; base < nb; base += step, half ^= 1) {
-        good = good_next; scale = scale_next;
-        if (base + step < nb) {
-            load_rows(base + step, half ^ 1);
-            asm volatile("cp.async.wait_group 1;" ::: "memory");
-        } else {
-            asm volatile("cp.async.wait_group 0;" ::: "memory");
-        }
+    int stage = 0;
+    for (int base = start; base < nb; base += step) {
+        asm volatile("cp.async.wait_group %0;" ::"n"(kFewStages - 1) : "memory");
         __syncwarp();
-        int mine = 0;                                         // the largest product of block base + lane
+        uint32_t a[2][W];
 #pragma unroll
-        for (int g = 0; g < 2; ++g) {
-            uint32_t a[2][W];
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int c = 0; c < W / 4; ++c) {
-                    const uint4 x = *reinterpret_cast<const uint4*>(piece(half, g * 16 + h * 8 + gid, tig + 4 * c));
-                    a[h][4 * c] = x.x; a[h][4 * c + 1] = x.y; a[h][4 * c + 2] = x.z; a[h][4 * c + 3] = x.w;
-                }
-            int best[2] = {INT32_MIN, INT32_MIN};
-#pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                int c[4] = {0, 0, 0, 0};
-#pragma unroll
-                for (int s = 0; s < W / 2; ++s) mma_s8(c, a[0][s], a[1][s], a[0][s + W / 2], a[1][s + W / 2], w[t][s], w[t][s + W / 2]);
-                best[0] = max(best[0], max(c[0], c[1]));
-                best[1] = max(best[1], max(c[2], c[3]));
+            for (int c = 0; c < W / 4; ++c) {
+                const uint4 x = *reinterpret_cast<const uint4*>(piece(stage, h * 8 + gid, tig + 4 * c));
+                a[h][4 * c] = x.x; a[h][4 * c + 1] = x.y; a[h][4 * c + 2] = x.z; a[h][4 * c + 3] = x.w;
             }
+        const float scale = s_scale[stage * kFewRows + (lane & 15)];
+        __syncwarp();                                         // the stage has been read
+        load_rows(base + kFewStages * step, stage, page_next);
+        page_next = page_of(base + (kFewStages + 1) * step);
+        int best[2] = {INT32_MIN, INT32_MIN};
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                int v = best[h];
-                v = max(v, __shfl_xor_sync(CB_FULL, v, 1));
-                v = max(v, __shfl_xor_sync(CB_FULL, v, 2));
-                v = __shfl_sync(CB_FULL, v, (lane & 7) * 4);
-                if ((lane >> 3) == 2 * g + h) mine = v;
-            }
+        for (int t = 0; t < NT; ++t) {
+            int c[4] = {0, 0, 0, 0};
+#pragma unroll
+            for (int s = 0; s < W / 2; ++s) mma_s8(c, a[0][s], a[1][s], a[0][s + W / 2], a[1][s + W / 2], w[t][s], w[t][s + W / 2]);
+            best[0] = max(best[0], max(c[0], c[1]));
+            best[1] = max(best[1], max(c[2], c[3]));
+        }
+        int mine = 0;                                         // lane l < 16: the largest product of block base + l
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            int v = best[h];
+            v = max(v, __shfl_xor_sync(CB_FULL, v, 1));
+            v = max(v, __shfl_xor_sync(CB_FULL, v, 2));
+            v = __shfl_sync(CB_FULL, v, (lane & 7) * 4);
+            if (((lane >> 3) & 1) == h) mine = v;
         }
         const int j = base + lane;
-        if (j < nb) {
+        if (lane < 16 && j < nb) {
             const uint32_t key = cb_score_key(mine, scale);
             if (ranks > 1) cb_cluster_store(key0 + 4u * (uint32_t)j, key);
             else s_key[j] = key;
-            if (!good) atomicCAS(p.status, 0u, (uint32_t)CB_ERR_INVALID_ARG);
         }
         __syncwarp();
+        stage = stage == kFewStages - 1 ? 0 : stage + 1;
     }
+    asm volatile("cp.async.wait_all;" ::: "memory");
     if (ranks > 1) {
         cb_cluster_arrive();
         cb_cluster_wait();
@@ -370,7 +382,7 @@ extern "C" cb_status cb_block_select(cb_ctx* ctx, const cb_block_select_args* a,
     int ctas = 1;
     while (ctas < 8 && (long long)p.B * p.Hkv * ctas * 2 <= ctx->num_sms && blocks > ctas * 128) ctas *= 2;
     if (nt == 0) return cb_select_launch_many(ctx, p, ctas, (cudaStream_t)stream);
-    const size_t smem = (size_t)p.key_words * 4 + (size_t)kFewThreads * 2 * c.head_dim;
+    const size_t smem = (size_t)p.key_words * 4 + (size_t)(kFewThreads / 32) * (c.head_dim == 128 ? kFewWarpBytes<128> : kFewWarpBytes<64>);
     const auto launch = [&](auto kernel, int which) -> cb_status {
         {
             std::lock_guard<std::mutex> lock(g_mutex);

@@ -659,8 +659,14 @@ __global__ void __launch_bounds__(kThreads, 1) cb_chunk_tc_kernel(const P p, con
                 };
                 auto store_lse = [&](float mx, float sum) {
                     if (row_valid && c0 == 0 && p.lse) {
-                        if constexpr (TREE) p.lse[((size_t)u->b * p.Hq + h) * p.T + token] = sum > 0.f ? (mx + log2f(sum)) * 0.6931471805599453f : 0.f;
-                        else p.lse[at_row] = (mx + log2f(sum)) * 0.6931471805599453f;
+                        size_t at = at_row;
+                        float e = (mx + log2f(sum)) * 0.6931471805599453f;
+                        if constexpr (TREE) {                 // [batch, heads, nodes]; head and node worked out again, which would be held through the tile loop
+                            const int tk = token_of(row), hd = (u->kh + (u->nrt == kTwoHeads ? l : 0)) * p.G + row - tk * p.G;
+                            at = (size_t)u->row0 * p.Hq + (size_t)hd * p.T + (2 * u->rg + (u->nrt == 2 ? l : 0)) * p.NPT + tk;
+                            e = sum > 0.f ? e : 0.f;          // (a row whose mask is empty, over no context)
+                        }
+                        p.lse[at] = e;
                     }
                 };
                 if (!whole && p.cs > 0) {

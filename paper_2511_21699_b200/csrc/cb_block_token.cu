@@ -138,7 +138,7 @@ __global__ void __launch_bounds__(32 * WARPS) cb_block_token_kernel(const CbList
     bool ok = true;
     for (int k = 0; k < count; ++k) {
         const uint32_t st = k % C::STAGES, kb = ring + st * 2 * C::PAGE, vb = kb + C::PAGE;
-        if (!(ok = mbar_wait(bars + 8 * st, (k / C::STAGES) & 1, s_abort, p.status))) break;
+        if (!(ok = __all_sync(CB_FULL, mbar_wait(bars + 8 * st, (k / C::STAGES) & 1, s_abort, p.status)))) break;   // (all lanes go on, or none)
         const int key0 = (pg0 + warp + k * WARPS) * 16;
         float sc[NT][4] = {};
 #pragma unroll

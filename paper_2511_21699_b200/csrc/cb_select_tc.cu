@@ -165,7 +165,7 @@ __global__ void __launch_bounds__(kManyThreads, 1) cb_select_many_kernel(const C
                     for (int e = (int)((mine - jobs) & 1u); e < count; e += 2) {
                         const uint32_t job = jobs + e;
                         const int m = e / halves, q = e - m * halves, cols = min(256, padded - q * 256);
-                        if (!(ok = mbar_wait(bar_full(mine), (job / 2) & 1, s_abort, p.status))) break;
+                        if (!(ok = __all_sync(CB_FULL, mbar_wait(bar_full(mine), (job / 2) & 1, s_abort, p.status)))) break;   // (all lanes go on, or none)
                         tc_fence_after();
                         int best = INT32_MIN;
                         // (64 columns under way at once, what lies behind the last query's 32 not looked at)

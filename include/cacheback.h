@@ -463,7 +463,7 @@ cb_status cb_chunk_attn(cb_ctx* ctx, const cb_chunk_attn_args* args, void* strea
  * sequence whose t exceeds max_pages.  A sequence with a negative length, or whose held is not in 0 .. max_pages, is left alone and
  * CB_ERR_INVALID_ARG recorded; a stack whose n_free is not in 0 .. num_pages, or that the pages given back would overfill, leaves everything as it
  * is and records the same.  Entries behind a row's pages and behind the top of the stack are not touched.  batch <= CB_MAX_ASSIGN,
- * num_pages <= 2^30.
+ * num_pages < 2^30.
  */
 enum { CB_MAX_ASSIGN = 16384 };
 cb_status cb_pages_assign(cb_ctx* ctx, const int32_t* want_len, int32_t* block_table, int32_t max_pages, int32_t* held, int32_t* free_pages,
@@ -503,7 +503,8 @@ cb_status cb_slot_map(cb_ctx* ctx, const cb_slot_map_args* args, void* stream);
  *   k_mean   int8 [num_pages, Hkv, D], k_scale float [num_pages, Hkv]     other pages' rows are left as they were
  * A head whose mean is not finite gets k_scale = +inf and zeros, which cb_block_select puts before all others.  A sequence with
  * from_len >= to_len has none; one with from_len < 0 is left alone and CB_ERR_INVALID_ARG recorded, one with to_len > max_pages * P CB_ERR_KV_FULL; a
- * block with a page outside the pool is left alone and CB_ERR_INVALID_ARG recorded.  batch <= CB_MAX_ASSIGN.
+ * block with a page outside the pool is left alone and CB_ERR_INVALID_ARG recorded.  batch <= CB_MAX_ASSIGN, batch * ceil(max_pages * P / block) < 2^30.
+ * Sequences that share pages (a common prefix) share their blocks' summaries: a block whose first page they share has to be the same in all of its pages and tokens.
  */
 typedef struct {
     const void* k_pool;

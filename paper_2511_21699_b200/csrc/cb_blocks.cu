@@ -326,6 +326,7 @@ extern "C" cb_status cb_block_summary(cb_ctx* ctx, const cb_block_summary_args* 
     CB_CHECK_ARG((((uintptr_t)a->k_pool | (uintptr_t)a->k_mean) & 15) == 0 && ((uintptr_t)a->k_scale & 3) == 0);
     const cb_config& c = ctx->cfg;
     if (c.page_size != 16 || c.batch > CB_MAX_ASSIGN) return CB_ERR_UNSUPPORTED;
+    if ((long long)c.batch * (((long long)a->max_pages * c.page_size + a->block - 1) / a->block) >= (long long)CB_SUM_CAP) return CB_ERR_UNSUPPORTED;   // (blocks are counted up to there)
     SummaryParams p = {};
     p.k_pool = (const __nv_bfloat16*)a->k_pool; p.table = a->block_table; p.from = a->from_len; p.to = a->to_len;
     p.mean = a->k_mean; p.scale = a->k_scale;

@@ -141,7 +141,7 @@ extern "C" cb_status cb_pages_assign(cb_ctx* ctx, const int32_t* want_len, int32
                                      int32_t num_pages, int32_t* n_free, void* stream) {
     CB_CHECK_ARG(ctx && want_len && block_table && held && free_pages && n_free && max_pages >= 1 && num_pages >= 1);
     const cb_config& c = ctx->cfg;
-    if (c.batch > CB_MAX_ASSIGN || num_pages > (int)CB_SUM_CAP) return CB_ERR_UNSUPPORTED;
+    if (c.batch > CB_MAX_ASSIGN || num_pages >= (int)CB_SUM_CAP) return CB_ERR_UNSUPPORTED;   // (a capped sum of needs exceeds all there can be)
     const size_t smem = (size_t)c.batch * 8;
     if (smem > 40 * 1024) CB_CUDA(cudaFuncSetAttribute(cb_pages_assign_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, CB_MAX_ASSIGN * 8));
     const long long entries = (long long)c.batch * max_pages;

@@ -107,3 +107,16 @@ def test_misaligned_pointers(cb):
         s = _lib.CbBlockSelectArgsC(base, base, None, base, base, base, base, base, 5, 9, 18, 64, 4, 1, 1, 0, 0)
         setattr(s, null, None)
         assert lib.cb_block_select(cb._h, C.byref(s), None) == _lib.CB_ERR_INVALID_ARG
+
+
+def test_numbers_above_what_is_counted(cb):
+    """Sums of pages and of blocks are counted below 2^30; what could exceed that is refused by its size alone, before anything is read."""
+    lib = _lib.load()
+    base = _t(1 << 10, dtype=torch.uint8).data_ptr()
+    unsupported = 6                                                          # CB_ERR_UNSUPPORTED
+    before = cb.launch_count()
+    assert lib.cb_pages_assign(cb._h, base, base, 9, base, base, 1 << 30, base, None) == unsupported
+    for block, most in ((16, 1 << 29), (64, (1 << 31) - 1)):                # (2 sequences of 2^29 blocks; 2^31 - 1 pages are 2^29 blocks)
+        a = _lib.CbBlockSummaryArgsC(base, base, base, base, base, base, most, 18, block)
+        assert lib.cb_block_summary(cb._h, C.byref(a), None) == unsupported
+    assert cb.launch_count() == before

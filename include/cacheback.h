@@ -205,7 +205,7 @@ cb_status cb_tree_add_branches(cb_ctx* ctx, const int32_t* branches, const int32
  *   block_table  int32 [batch, max_pages]       page id of the j-th page of each sequence
  *   ctx_len      int32 [batch]                  cached tokens per sequence (<= max_pages * P)
  *   k_tree,v_tree bf16 [batch, T, Hkv, D]       keys / values of the tree tokens themselves
- *   tree_mask    uint32 [batch, T, W], n_nodes int32 [batch]   as written by cb_draft_tree
+ *   tree_mask    uint32 [batch, T, W], n_nodes int32 [batch]   as written by cb_draft_tree: node 0 is in the masks of all nodes
  *   out          bf16 [batch, T, Hq, D]         rows >= n_nodes are written as zero
  *   lse          float [batch, Hq, T] or NULL   natural-log sum of exponentials per row (0 for padding)
  *   max_ctx      host upper bound on every ctx_len (0 = max_pages * P); sizes the grid and, with few units, names the page-table entry of
@@ -561,7 +561,8 @@ cb_status cb_block_select(cb_ctx* ctx, const cb_block_select_args* args, void* s
  * Attention over the selected blocks.
  *   cb_block_attn       cb_chunk_attn in which row q_start[b] + i sees, of the ctx_len[b] cached tokens, only those in its kv head's blocks, and
  *                       the chunk's own tokens up to its own
- *   cb_block_tree_attn  cb_tree_attn in which the cached context is that of the kv head's blocks
+ *   cb_block_tree_attn  cb_tree_attn in which the cached context is that of the kv head's blocks; masks of any form (a row that sees no token and no
+ *                       node is zero, its lse too)
  * Arguments, outputs, errors and alignment are those of the dense calls (max_ctx still bounds all of a sequence's tokens); blocks int32 [batch, Hkv,
  * n_select] is as cb_block_select leaves it for the same ctx_len and block: with nb = ceil(ctx_len / block) > n_select a list names n_select
  * blocks below nb, the newest one last; with fewer its first nb entries are 0 .. nb - 1.  Other lists give rows of no meaning; a block that does

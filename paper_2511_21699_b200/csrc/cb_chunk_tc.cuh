@@ -526,7 +526,9 @@ __global__ void __launch_bounds__(kThreads, 1) cb_chunk_tc_kernel(const P p, con
                         return all_vis ? make_p_of(mu, std::false_type{}) : make_p_of(mu, std::true_type{});
                     };
                     float lt = make_p(m_used == -INFINITY ? 0.f : m_used);
-                    if (pair_sync(row_valid && !(lt <= kRowSumLimit), 0)) {          // rows that do not exist hold anything: they never ask
+                    // (A tree's row may see none of its first 32 keys and others behind them: its sum against 0 stands for nothing, it needs a reference.)
+                    const bool none = TREE && m_used == -INFINITY && (vm[0] | vm[1]) != 0u;
+                    if (pair_sync(row_valid && (none || !(lt <= kRowSumLimit)), 0)) {          // rows that do not exist hold anything: they never ask
                         // pass 1: the row's maximum over all its visible scores (both threads of the row take it)
                         const int kv = all_vis ? CB_KT : (row_valid ? (TREE ? u->ctx : limit) - i * CB_KT : 0);
                         float mx = -INFINITY;

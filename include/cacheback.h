@@ -563,7 +563,9 @@ cb_status cb_block_select(cb_ctx* ctx, const cb_block_select_args* args, void* s
  *                       the chunk's own tokens up to its own
  *   cb_block_tree_attn  cb_tree_attn in which the cached context is that of the kv head's blocks; masks of any form (a row that sees no token and no
  *                       node is zero, its lse too)
- * Arguments, outputs, errors and alignment are those of the dense calls (max_ctx still bounds all of a sequence's tokens); blocks int32 [batch, Hkv,
+ * Arguments, outputs, errors and alignment are those of the dense calls (max_ctx bounds what it bounds there: a chunk's cached and new tokens, a tree's
+ * cached ones).  A tree whose n_nodes is not in 0 .. T or whose ctx_len is negative (CB_ERR_INVALID_ARG recorded), or whose ctx_len exceeds max_ctx or
+ * max_pages * P (CB_ERR_KV_FULL), gets zeros as if it had no nodes; without nodes its ctx_len is not looked at.  blocks int32 [batch, Hkv,
  * n_select] is as cb_block_select leaves it for the same ctx_len and block: with nb = ceil(ctx_len / block) > n_select a list names n_select
  * blocks below nb, the newest one last; with fewer its first nb entries are 0 .. nb - 1.  Other lists give rows of no meaning; a block that does
  * not exist, or a page outside the pool, reads as zeros.

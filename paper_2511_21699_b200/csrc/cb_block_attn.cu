@@ -22,7 +22,11 @@ __global__ void __launch_bounds__(32 * kWarps) cb_block_cc_kernel(const P p) {
     const long long rows = (long long)p.n_rows * p.Hq;
     if (item >= rows) {                                       // behind the rows' warps, a sequence per lane: what is wrong with it
         const long long b = (item - rows) * 32 + lane;
-        const int error = !TREE && b < p.B ? cb_chunk_seq(p, (int)b).error : 0;
+        int error = 0;
+        if (b < p.B) {
+            if constexpr (TREE) error = cb_tree_error(p, (int)b);
+            else error = cb_chunk_seq(p, (int)b).error;
+        }
         if (error) atomicCAS(p.status, 0u, (uint32_t)error);
         return;
     }
@@ -30,9 +34,9 @@ __global__ void __launch_bounds__(32 * kWarps) cb_block_cc_kernel(const P p) {
     int b, ctx, i, own;                                       // own: new tokens (nodes) that the row may see
     if constexpr (TREE) {
         b = row / p.T; i = row % p.T;
-        ctx = cb_tree_ctx(p, b);
-        own = min(max(p.n_nodes[b], 0), p.T);
-        if (i >= own) {                                       // padding
+        own = cb_tree_nodes(p, b);
+        ctx = p.ctx_len[b];
+        if (i >= own) {                                       // padding, or a sequence out of its bounds
             for (int c = 0; c < C; ++c) p.out[((size_t)row * p.Hq + h) * D + lane + 32 * c] = __float2bfloat16_rn(0.f);
             if (p.lse && lane == 0) p.lse[((size_t)b * p.Hq + h) * p.T + i] = 0.f;
             return;

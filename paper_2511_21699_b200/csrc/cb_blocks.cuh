@@ -40,9 +40,19 @@ __device__ __forceinline__ CbChunkSeq cb_chunk_seq(const CbListParams& p, int b)
     if (s.n > 0) s.ctx = cb_seen(p.l, s.ctx);
     return s;
 }
-__device__ __forceinline__ int cb_tree_ctx(const CbListTreeParams& p, int b) { return min(max(p.ctx_len[b], 0), p.max_keys); }
+// Nodes of a tree, 0 where its lengths are out of their bounds, and what is wrong with them then (0: there are none).
+__device__ __forceinline__ int cb_tree_nodes(const CbListTreeParams& p, int b) {
+    const int n = p.n_nodes[b];
+    return (uint32_t)n <= (uint32_t)p.T && (uint32_t)p.ctx_len[b] <= (uint32_t)p.max_keys ? n : 0;
+}
+__device__ __forceinline__ int cb_tree_error(const CbListTreeParams& p, int b) {
+    const int n = p.n_nodes[b];
+    if (n == 0 || cb_tree_nodes(p, b) > 0) return 0;
+    return n > 0 && n <= p.T && p.ctx_len[b] > p.max_keys ? CB_ERR_KV_FULL : CB_ERR_INVALID_ARG;
+}
+// (Errors are looked for where rows of zeros are written: held through the walk over the units they cost 24 bytes of spills a thread, and 0.5 to 1% of the time.)
 __device__ __forceinline__ CbChunkSeq cb_chunk_seq(const CbListTreeParams& p, int b) {
-    return {b * p.T, min(max(p.n_nodes[b], 0), p.T), cb_seen(p.l, cb_tree_ctx(p, b)), 0};
+    return {b * p.T, cb_tree_nodes(p, b), cb_seen(p.l, p.ctx_len[b]), 0};
 }
 
 cb_status cb_block_launch_tensor(cb_ctx* ctx, const CbListParams& p, cudaStream_t st);

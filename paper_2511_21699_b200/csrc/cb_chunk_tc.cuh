@@ -184,8 +184,7 @@ __global__ void __launch_bounds__(kThreads, 1) cb_chunk_tc_kernel(const P p, con
                 const int32_t* bt = p.block_table + (size_t)u->b * p.max_pages;
                 const int nct = TREE ? u->tiles - 1 : 0;      // a tree's own keys are its last tile
                 int nb = 0;
-                if constexpr (TREE) nb = cb_blocks_of(cb_tree_ctx(p, u->b), p.l.shift);
-                else if constexpr (LISTS) nb = cb_blocks_of(p.ctx_len[u->b], p.l.shift);
+                if constexpr (LISTS) nb = cb_blocks_of(p.ctx_len[u->b], p.l.shift);
                 uint32_t seq = (uint32_t)u->seq0 + (isV ? 1u : 0u);
                 // the page number is fetched one tile ahead of the copy that depends on it; out of the pool, the copy fills zeros
                 auto page_of = [&](int i, int h) {
@@ -404,9 +403,13 @@ __global__ void __launch_bounds__(kThreads, 1) cb_chunk_tc_kernel(const P p, con
             return pair_or(pair_id, v);
         };
         bool ok = true;
-        if constexpr (TREE) {                                 // the rows of nodes that do not exist are zero
+        if constexpr (TREE) {                                 // the rows of nodes that do not exist are zero, and those of a sequence out of its bounds
             for (int b = cta; b < p.B; b += gridDim.x) {
-                const int n = min(max(p.n_nodes[b], 0), p.T), pieces = (p.T - n) * p.Hq * (D / 8);
+                const int n = cb_tree_nodes(p, b), pieces = (p.T - n) * p.Hq * (D / 8);
+                if (n == 0 && sw == 0 && lane == 0) {
+                    const int error = cb_tree_error(p, b);
+                    if (error) atomicCAS(p.status, 0u, (uint32_t)error);
+                }
                 uint4* const at = reinterpret_cast<uint4*>(p.out + ((size_t)b * p.T + n) * p.Hq * D);
                 for (int k = sw * 32 + lane; k < pieces; k += 512) at[k] = make_uint4(0, 0, 0, 0);
                 if (p.lse)

@@ -357,7 +357,7 @@ extern "C" cb_status cb_block_select(cb_ctx* ctx, const cb_block_select_args* a,
     CB_CHECK_ARG(a->k_mean && a->k_scale && a->block_table && a->ctx_len && a->blocks && a->max_pages >= 1 && a->num_pages >= 1);
     CB_CHECK_ARG(a->block == 16 || a->block == 32 || a->block == 64 || a->block == 128);
     CB_CHECK_ARG(a->n_rows >= 0 && a->max_chunk >= 0 && a->max_ctx >= 0 && (a->q || (a->q_start && a->n_rows == 0)));
-    CB_CHECK_ARG(a->n_first >= 0 && a->n_last >= 1 && a->n_select <= CB_MAX_SELECT && a->n_first <= a->n_select - a->n_last);
+    CB_CHECK_ARG(a->n_first >= 0 && a->n_last >= 1 && a->n_select >= 1 && a->n_select <= CB_MAX_SELECT && a->n_first <= a->n_select - a->n_last);
     CB_CHECK_ARG((((uintptr_t)a->q | (uintptr_t)a->k_mean) & 15) == 0 && ((uintptr_t)a->k_scale & 3) == 0);
     const cb_config& c = ctx->cfg;
     if (c.page_size != 16) return CB_ERR_UNSUPPORTED;

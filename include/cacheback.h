@@ -531,7 +531,8 @@ cb_status cb_block_summary(cb_ctx* ctx, const cb_block_summary_args* args, void*
  *   ctx_len  int32 [batch]   cached tokens before the chunk or the tree
  *   blocks   int32 [batch, Hkv, n_select]   by rising number; -1 behind the last where nb < n_select; all -1 where there are no rows
  *   n_first >= 0, n_last >= 1, n_first + n_last <= n_select <= CB_MAX_SELECT
- *   max_chunk  host upper bound on a chunk's rows (0 = n_rows), max_ctx on every ctx_len (0 = max_pages * P); max_ctx / block <= 16,384
+ *   max_chunk  host upper bound on a chunk's rows (0 = n_rows; more than 20,000,000 may be turned away as if it were above the bound), max_ctx on
+ *              every ctx_len (0 = max_pages * P); max_ctx / block <= 16,384
  * A sequence whose rows or ctx_len are out of their bounds (q_start's range, n_nodes, max_chunk; negative ctx_len: CB_ERR_INVALID_ARG; ctx_len > max_ctx:
  * CB_ERR_KV_FULL) gets -1 throughout.  A block whose first page lies outside the pool scores as if k_scale were 0, CB_ERR_INVALID_ARG recorded.  Queries
  * are finite.

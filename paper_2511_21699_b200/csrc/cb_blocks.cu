@@ -375,6 +375,9 @@ extern "C" cb_status cb_block_select(cb_ctx* ctx, const cb_block_select_args* a,
     if (blocks > 16384) return CB_ERR_UNSUPPORTED;            // (keys of all blocks beside the tiles in shared memory)
     p.key_words = (blocks + 3) & ~3;
     p.g_inv = p.G > 1 ? 0xFFFFFFFFu / (uint32_t)p.G + 1u : 0u;
+    // Row and head of a chunk's query x are exact while x times what g_inv is too large by stays below 2^32; longer chunks are turned away with those above the caller's bound.
+    const uint32_t over = p.g_inv * (uint32_t)p.G;            // G g_inv - 2^32, less than G
+    if (over) p.max_chunk = std::min(p.max_chunk, (int)std::min<uint32_t>(0xFFFFFFFFu / over / (uint32_t)p.G, INT32_MAX));
     if (!p.q_start && (long long)p.B * p.T > 0x7FFFFFFFll) return CB_ERR_UNSUPPORTED;
     // Up to 16 queries (rows x heads of the group) lie in a warp's registers; more are a matter of the tensor pipe, and of 128 blocks a tile.  With few units a
     // cluster shares each one's blocks: as many CTAs as there are SMs for and tiles to keep them busy.

@@ -11,7 +11,7 @@ struct CbSelectParams {
     int32_t* out;
     int B, T, Hq, Hkv, G, P, max_pages, num_pages, n_rows, max_chunk, max_ctx;
     int shift, K, n_first, n_last;
-    uint32_t g_inv;           // x / G = __umulhi(x, g_inv) for x < 2^28; 0: G is 1
+    uint32_t g_inv;           // x / G = __umulhi(x, g_inv) for the queries x of chunks up to max_chunk; 0: G is 1
     int key_words;            // words of shared memory for the keys of all blocks, a multiple of 4
     uint32_t* status;
 };

@@ -1,7 +1,8 @@
 """Thin Python binding of the C-ABI library: argument marshalling only.
 
 Tensors are torch CUDA tensors (device memory and streams are torch's); every step of the path runs in
-the library's kernels.  Method names mirror the C entry points.  The calls of a decoding loop are marshalled by the compiled
+the library's kernels.  With `stream` (a torch stream, or anything that has its cuda_stream) a call is queued there instead of on the current one: the tensors that it is given have to be
+ready there and are the caller's to keep until it has run; those that it makes are safe on both.  Method names mirror the C entry points.  The calls of a decoding loop are marshalled by the compiled
 module _binding (csrc/cb_binding.cpp), the others by ctypes here.
 """
 import ctypes as C
@@ -34,6 +35,23 @@ def _ptr(t, dtype=None):
 
 def _stream(stream):
     return (stream if stream is not None else torch.cuda.current_stream()).cuda_stream
+
+
+def _made(make, stream, device):
+    """The tensors that a call writes where it is given none: make().  On a stream other than the current one they come from that stream's memory, which nothing that is queued on the
+    current one still uses, and are not reused before what the current one does with them until they are freed."""
+    if stream is None:
+        return make()
+    on = stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(stream.cuda_stream, device=device)
+    now = torch.cuda.current_stream(device)
+    if on == now:
+        return make()
+    with torch.cuda.stream(on):
+        res = make()
+    for t in res.values() if isinstance(res, dict) else res if isinstance(res, tuple) else (res,):
+        if t.is_cuda:                                                        # (others are refused where the call looks at them)
+            t.record_stream(now)
+    return res
 
 
 _BOUND = ("cb_reset", "cb_update", "cb_update_bulk", "cb_draft_tree", "cb_update_draft_tree", "cb_tree_attn", "cb_accept",
@@ -82,8 +100,8 @@ def cb_accept_static(tree, logits, max_depth, res=None, stream=None):
         raise CachebackError("logits must be [batch, max_nodes, vocab] with a uniform row stride")
     if res is None:
         i32 = dict(dtype=torch.int32, device=logits.device)
-        res = dict(n_accept=torch.empty(B, **i32), accept_nodes=torch.empty(B, max_depth, **i32),
-                   out_tokens=torch.empty(B, max_depth + 1, **i32), target_ids=torch.empty(B, T, **i32))
+        res = _made(lambda: dict(n_accept=torch.empty(B, **i32), accept_nodes=torch.empty(B, max_depth, **i32),
+                                 out_tokens=torch.empty(B, max_depth + 1, **i32), target_ids=torch.empty(B, T, **i32)), stream, logits.device)
     _check(lib.cb_accept_static(B, T, max_depth, V, _ptr(tree["tokens"], torch.int32), _ptr(tree["parent"], torch.int32),
                                 _ptr(tree["depth"], torch.int32), _ptr(tree["n_nodes"], torch.int32), logits.data_ptr(), dtype,
                                 logits.stride(1), _ptr(res["n_accept"], torch.int32), _ptr(res["accept_nodes"], torch.int32),
@@ -128,7 +146,7 @@ class FrozenTable:
         nbytes = C.c_size_t(0)
         _check(self.lib.cb_frozen_build_bytes(C.byref(self.cfg), n, C.byref(nbytes)), "cb_frozen_build_bytes")
         with torch.cuda.device(self.device):
-            scratch = torch.empty(nbytes.value + 256, dtype=torch.uint8, device=self.device)
+            scratch = _made(lambda: torch.empty(nbytes.value + 256, dtype=torch.uint8, device=self.device), stream, self.device)
             sp = (scratch.data_ptr() + 255) // 256 * 256
             _check(self.lib.cb_frozen_build(C.byref(self.cfg), _ptr(corpus, torch.int32), n, self.ptr, self.bytes, sp, nbytes.value,
                                             _stream(stream)), "cb_frozen_build")
@@ -222,13 +240,13 @@ class Cacheback:
                     mask=torch.empty(B, T, self.W, **i32), n_nodes=torch.empty(B, **i32))
 
     def cb_draft_tree(self, tokens, seq_len, tree=None, stream=None):
-        tree = tree if tree is not None else self.alloc_tree()
+        tree = tree if tree is not None else _made(self.alloc_tree, stream, self.device)
         self._host.draft_tree(self._h, tokens, seq_len, tree, stream)
         return tree
 
     def cb_update_draft_tree(self, tokens, n_old, n_new, tree=None, stream=None):
         """cb_update(tokens, n_old, n_new) and cb_draft_tree(tokens, n_new) in one launch."""
-        tree = tree if tree is not None else self.alloc_tree()
+        tree = tree if tree is not None else _made(self.alloc_tree, stream, self.device)
         self._host.update_draft_tree(self._h, tokens, n_old, n_new, tree, stream)
         return tree
 
@@ -244,7 +262,7 @@ class Cacheback:
     def cb_tree_attn(self, q, k_pool, v_pool, block_table, ctx_len, k_tree, v_tree, tree_mask, n_nodes, out=None,
                      lse=None, max_ctx=0, scale=0.0, stream=None):
         if out is None:
-            out = torch.empty_like(q)
+            out = _made(lambda: torch.empty_like(q), stream, self.device)
         self._host.tree_attn(self._h, q, k_pool, v_pool, block_table, ctx_len, k_tree, v_tree, tree_mask, n_nodes, out, lse, int(max_ctx),
                              float(scale), stream)
         return out
@@ -259,14 +277,14 @@ class Cacheback:
                     out_tokens=torch.empty(B, Dm + 1, **i32), target_ids=torch.empty(B, self.cfg.max_nodes, **i32))
 
     def cb_accept(self, tree, logits=None, target_ids=None, res=None, stream=None):
-        res = res if res is not None else self.alloc_accept()
+        res = res if res is not None else _made(self.alloc_accept, stream, self.device)
         self._host.accept(self._h, tree, logits, target_ids, res, stream)
         return res
 
     def cb_accept_update_draft_tree(self, tree, logits, tokens, seq_len, next_tree=None, res=None, stream=None):
         """cb_accept on `tree` and `logits`, the emitted tokens appended to `tokens` (seq_len advanced in place), then cb_update
         and cb_draft_tree into next_tree (default: the same arrays as `tree`), in one launch."""
-        res = res if res is not None else self.alloc_accept()
+        res = res if res is not None else _made(self.alloc_accept, stream, self.device)
         next_tree = next_tree if next_tree is not None else tree
         self._host.accept_update_draft_tree(self._h, tree, logits, tokens, seq_len, next_tree, res, stream)
         return res
@@ -278,7 +296,7 @@ class Cacheback:
         rotation of q and k, k and v into the pages behind the ctx_len[b] cached tokens.  q, k, v [rows, heads, head_dim], each row
         contiguous (they may be parts of one projection).  Returns the queries [rows, n_q_heads, head_dim]; ctx_len is not advanced."""
         if q_out is None:
-            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            q_out = _made(lambda: torch.empty(q.shape, dtype=q.dtype, device=q.device), stream, self.device)
         self._host.chunk_append(self._h, self._shape, q, k, v, q_norm, k_norm, eps, rope, interleaved, q_start, ctx_len, k_pool, v_pool, block_table,
                                 q_out, stream)
         return q_out
@@ -288,7 +306,7 @@ class Cacheback:
         keys and values into the pages.  max_chunk, max_ctx: host upper bounds on the new tokens of a sequence and on its cached and
         new tokens together (0: not known).  scale: positive, 0 selects 1 / sqrt(head_dim)."""
         if out is None:
-            out = torch.empty_like(q)
+            out = _made(lambda: torch.empty_like(q), stream, self.device)
         self._host.chunk_attn(self._h, self._shape, q, k_pool, v_pool, block_table, q_start, ctx_len, out, lse, max_chunk, max_ctx, scale, stream)
         return out
 
@@ -297,7 +315,7 @@ class Cacheback:
         """The norm and rotation of cb_chunk_append for the nodes of a draft tree (row b * max_nodes + i is node i of sequence b, at
         position ctx_len[b] + depth): the q, k_tree and v_tree that cb_tree_attn takes, rows behind n_nodes zero."""
         c = self.cfg
-        new = lambda heads: torch.empty(c.batch, c.max_nodes, heads, c.head_dim, dtype=torch.bfloat16, device=self.device)
+        new = lambda heads: _made(lambda: torch.empty(c.batch, c.max_nodes, heads, c.head_dim, dtype=torch.bfloat16, device=self.device), stream, self.device)
         q_out = q_out if q_out is not None else new(c.n_q_heads)
         k_out = k_out if k_out is not None else new(c.n_kv_heads)
         v_out = v_out if v_out is not None else new(c.n_kv_heads)
@@ -317,7 +335,7 @@ class Cacheback:
         (logprobs is not written)."""
         if res is None:
             n = rows if rows is not None else (tokens if tokens is not None else logits)
-            res = self._alloc_logprobs((int(n.shape[0]),), top_k)
+            res = _made(lambda: self._alloc_logprobs((int(n.shape[0]),), top_k), stream, self.device)
         self._host.logprobs(self._h, self._shape, logits, tokens, rows, top_k, res, stream)
         return res
 
@@ -325,7 +343,7 @@ class Cacheback:
         """The same for the tokens that cb_accept emitted (`accepted`: its result), from the logits that it was given: outputs
         [batch, max_depth + 1], padding behind the last emitted token."""
         if res is None:
-            res = self._alloc_logprobs((self.cfg.batch, self.cfg.max_depth + 1), top_k)
+            res = _made(lambda: self._alloc_logprobs((self.cfg.batch, self.cfg.max_depth + 1), top_k), stream, self.device)
         self._host.accept_logprobs(self._h, self._shape, logits, accepted, top_k, res, stream)
         return res
 
@@ -340,7 +358,7 @@ class Cacheback:
         positions and seqs int32, each [n_rows]."""
         if res is None:
             new = lambda t: torch.empty(n_rows, dtype=t, device=self.device)
-            res = dict(slots=new(torch.int64), positions=new(torch.int32), seqs=new(torch.int32))
+            res = _made(lambda: dict(slots=new(torch.int64), positions=new(torch.int32), seqs=new(torch.int32)), stream, self.device)
         self._host.slot_map(self._h, self._shape, q_start, ctx_len, block_table, num_pages, n_rows, res, stream)
         return res
 
@@ -361,7 +379,7 @@ class Cacheback:
         [batch, n_kv_heads, n_select], -1 behind the last.  The queries are a chunk's (q [rows, heads, head_dim] and q_start) or a tree's (q [batch, max_nodes,
         heads, head_dim] and n_nodes).  The n_first first and the n_last newest blocks are always among them."""
         if blocks is None:
-            blocks = torch.empty(self.cfg.batch, self.cfg.n_kv_heads, n_select, dtype=torch.int32, device=self.device)
+            blocks = _made(lambda: torch.empty(self.cfg.batch, self.cfg.n_kv_heads, n_select, dtype=torch.int32, device=self.device), stream, self.device)
         self._host.block_select(self._h, self._shape, q, k_mean, k_scale, block_table, ctx_len, q_start, n_nodes, block, n_select, n_first, n_last, max_chunk,
                                 max_ctx, blocks, stream)
         return blocks
@@ -370,7 +388,7 @@ class Cacheback:
                       stream=None):
         """cb_chunk_attn over the selected blocks of the cached tokens and the chunk's own ones.  blocks: of cb_block_select, for the same ctx_len."""
         if out is None:
-            out = torch.empty_like(q)
+            out = _made(lambda: torch.empty_like(q), stream, self.device)
         self._host.block_attn(self._h, self._shape, q, k_pool, v_pool, block_table, q_start, ctx_len, out, lse, max_chunk, max_ctx, scale, blocks, block,
                               stream)
         return out
@@ -379,7 +397,7 @@ class Cacheback:
                            max_ctx=0, scale=0.0, stream=None):
         """cb_tree_attn over the selected blocks of the cached tokens and the tree's nodes."""
         if out is None:
-            out = torch.empty_like(q)
+            out = _made(lambda: torch.empty_like(q), stream, self.device)
         self._host.block_tree_attn(self._h, self._shape, q, k_pool, v_pool, block_table, ctx_len, k_tree, v_tree, tree_mask, n_nodes, out, lse, max_ctx,
                                    scale, blocks, block, stream)
         return out

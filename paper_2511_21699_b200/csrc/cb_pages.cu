@@ -5,9 +5,10 @@
 // sum of needs passes j.  So all moves are independent: a thread finds both sequences of a move by two searches in shared memory.  Pages given back
 // that nobody takes are pushed above the old top, pages taken from the stack lie below it, rows that are read belong to sequences that shrink and rows
 // that are written to such that grow: no move touches what another one reads.  held and n_free, which all CTAs read, are written by the one that counted itself
-// last behind that.  How many moves there are is known on the device only: a table of up to 65,536 entries gets one CTA (a step's few moves: the count would cost
-// more than it shares), a larger one as many as it has 2,048 entries, one an SM at most.  Round trips bound it: 3.5 us a call for 32 sequences of which half
-// take a page, 5.5 for 512 sequences that take or give back 133,000 (a cluster of eight CTAs: 6.6 and 24).
+// last behind that.  How many moves there are is known on the device only: a table of up to 16,384 entries gets one CTA, a larger one as many
+// as it has 2,048 entries, one an SM at most.  (A step of 32 sequences, one CTA against that many: 3.8 and 4.0 us with 16,384 entries, 3.8 and 3.9 with 32,768; calls that move a
+// quarter of the table: 6.0 and 3.9, 8.9 and 4.1, with 65,536 entries 15 and 4.0.  With a CTA for 8,192 entries 5.0, for 512 as for 2,048.)  Round trips bound it: 3.5 us a call for
+// 32 sequences of which half take a page, 5.5 for 512 sequences that take or give back 133,000 (a cluster of eight CTAs: 6.6 and 24).
 //
 // cb_slot_map.  A thread per row: the sequence by a search in the block's copy of q_start, then its length and page.  The launch bounds it: 3.1 us a call for 32 rows and
 // for 66,000.
@@ -145,7 +146,7 @@ extern "C" cb_status cb_pages_assign(cb_ctx* ctx, const int32_t* want_len, int32
     const size_t smem = (size_t)c.batch * 8;
     if (smem > 40 * 1024) CB_CUDA(cudaFuncSetAttribute(cb_pages_assign_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, CB_MAX_ASSIGN * 8));
     const long long entries = (long long)c.batch * max_pages;
-    const unsigned ctas = entries <= 65536 ? 1u : (unsigned)std::min<long long>(entries / 2048, ctx->num_sms);
+    const unsigned ctas = entries <= 16384 ? 1u : (unsigned)std::min<long long>(entries / 2048, ctx->num_sms);
     CB_CUDA(cb_launch_pdl(cb_pages_assign_kernel, dim3(ctas), dim3(kPageThreads), smem, (cudaStream_t)stream, (int)c.batch, (int)c.page_size, (int)max_pages,
                           (int)num_pages, want_len, block_table, held, free_pages, n_free, ctx->d_ticket, ctx->d_status));
     cb_count_launch(1);

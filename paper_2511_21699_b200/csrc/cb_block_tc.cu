@@ -10,7 +10,7 @@ namespace {
 template <typename P, typename Encode>
 cb_status launch(cb_ctx* ctx, const P& given, cudaStream_t st, long long own, Encode&& more) {
     P p = given;
-    if (p.P != 16 || p.num_pages >= 1 << 29) return CB_ERR_UNSUPPORTED;   // (a page's coordinate is twice its number)
+    if (p.num_pages >= 1 << 29) return CB_ERR_UNSUPPORTED;   // (a page's coordinate is twice its number)
     chunk_split(ctx, p, std::min<long long>(p.max_keys, (long long)p.l.n_select << p.l.shift) + own);
     MapsOf<P> maps;
     if (!encode_pool(&maps.k, p.k_pool, p) || !encode_pool(&maps.v, p.v_pool, p) || !encode_queries(&maps.q, p) || !more(&maps)) return CB_ERR_CUDA;

@@ -307,7 +307,7 @@ cb_status launch_warps(const cb_ctx* ctx, const CbListParams& p, bool resident, 
 
 cb_status cb_block_launch_token(cb_ctx* ctx, const CbListParams& given, cudaStream_t st) {
     CbListParams p = given;
-    if (p.P != 16 || p.num_pages >= 1 << 29) return CB_ERR_UNSUPPORTED;   // (a page's coordinate is twice its number)
+    if (p.num_pages >= 1 << 29) return CB_ERR_UNSUPPORTED;   // (a page's coordinate is twice its number)
     p.g_inv = 65536u / (uint32_t)p.G + 1u;                    // x / G = x * g_inv >> 16 for x < 256
     const long long units = (long long)p.B * p.Hkv, pages = (std::min<long long>(p.max_keys, ((long long)p.l.n_select << p.l.shift) + p.max_chunk) + 15) / 16;
     // A cluster shares a unit while all CTAs find an SM of their own and four pages each (8 sequences of 8 kv heads, 2,048 keys: 11.1 us with 128 CTAs, 14.3 with 64, 28 with

@@ -325,7 +325,7 @@ extern "C" cb_status cb_block_summary(cb_ctx* ctx, const cb_block_summary_args* 
     CB_CHECK_ARG(a->block == 16 || a->block == 32 || a->block == 64 || a->block == 128);
     CB_CHECK_ARG((((uintptr_t)a->k_pool | (uintptr_t)a->k_mean) & 15) == 0 && ((uintptr_t)a->k_scale & 3) == 0);
     const cb_config& c = ctx->cfg;
-    if (c.page_size != 16 || c.batch > CB_MAX_ASSIGN) return CB_ERR_UNSUPPORTED;
+    if (c.batch > CB_MAX_ASSIGN) return CB_ERR_UNSUPPORTED;
     if ((long long)c.batch * (((long long)a->max_pages * c.page_size + a->block - 1) / a->block) >= (long long)CB_SUM_CAP) return CB_ERR_UNSUPPORTED;   // (blocks are counted up to there)
     SummaryParams p = {};
     p.k_pool = (const __nv_bfloat16*)a->k_pool; p.table = a->block_table; p.from = a->from_len; p.to = a->to_len;
@@ -360,7 +360,6 @@ extern "C" cb_status cb_block_select(cb_ctx* ctx, const cb_block_select_args* a,
     CB_CHECK_ARG(a->n_first >= 0 && a->n_last >= 1 && a->n_select >= 1 && a->n_select <= CB_MAX_SELECT && a->n_first <= a->n_select - a->n_last);
     CB_CHECK_ARG((((uintptr_t)a->q | (uintptr_t)a->k_mean) & 15) == 0 && ((uintptr_t)a->k_scale & 3) == 0);
     const cb_config& c = ctx->cfg;
-    if (c.page_size != 16) return CB_ERR_UNSUPPORTED;
     CbSelectParams p = {};
     p.q = (const __nv_bfloat16*)a->q; p.q_start = a->q_start; p.n_nodes = a->n_nodes; p.mean = a->k_mean; p.scale = a->k_scale;
     p.table = a->block_table; p.ctx_len = a->ctx_len; p.out = a->blocks;

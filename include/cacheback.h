@@ -497,8 +497,9 @@ cb_status cb_slot_map(cb_ctx* ctx, const cb_slot_map_args* args, void* stream);
  *
  * cb_block_summary: the summaries of the blocks that new tokens touch, after their keys are in the pages (cb_chunk_append, cb_kv_commit).  For
  * every block that holds one of the positions from_len[b] .. to_len[b] - 1 of sequence b, over its tokens below to_len[b], m = sum of a head's keys / tokens:
- *   k_scale = max |m| / 127,   k_mean[d] = m[d] * 127 / max |m| rounded to the nearest whole number (half way: to the even one)
- * each operation in 64 bits, where the sum is exact, and so independent of any order of addition.  They are stored with the block's first page.
+ *   k_scale = max |m| / 127,   k_mean[d] = m[d] * 127 / max(max |m|, 1e-30) rounded to the nearest whole number (half way: to the even one)
+ * each operation in 64 bits.  The sum is exact there, and so independent of any order of addition, unless the exponents of a channel's keys lie more than 38
+ * apart; then too it is taken in one order whatever the call: equal keys give equal bits.  They are stored with the block's first page.
  *   k_pool   bf16 [num_pages, P, Hkv, D];  block_table int32 [batch, max_pages];  from_len, to_len int32 [batch]
  *   k_mean   int8 [num_pages, Hkv, D], k_scale float [num_pages, Hkv]     other pages' rows are left as they were
  * A head whose mean is not finite gets k_scale = +inf and zeros, which cb_block_select puts before all others.  A sequence with
@@ -532,7 +533,9 @@ cb_status cb_block_summary(cb_ctx* ctx, const cb_block_summary_args* args, void*
  *   blocks   int32 [batch, Hkv, n_select]   by rising number; -1 behind the last where nb < n_select; all -1 where there are no rows
  *   n_first >= 0, n_last >= 1, n_first + n_last <= n_select <= CB_MAX_SELECT
  *   max_chunk  host upper bound on a chunk's rows (0 = n_rows; more than 20,000,000 may be turned away as if it were above the bound), max_ctx on
- *              every ctx_len (0 = max_pages * P); max_ctx / block <= 16,384
+ *              every ctx_len (0 = max_pages * P); max_ctx / block <= 16,384.  max_chunk is worth giving: with at most 16 queries a kv head, max_chunk
+ *              * Hq / Hkv, units are taken by a kernel for few queries (64 single tokens: a third of the time).  One long chunk takes all
+ *              sequences of its call to the other kernel.
  * A sequence whose rows or ctx_len are out of their bounds (q_start's range, n_nodes, max_chunk; negative ctx_len: CB_ERR_INVALID_ARG; ctx_len > max_ctx:
  * CB_ERR_KV_FULL) gets -1 throughout.  A block whose first page lies outside the pool scores as if k_scale were 0, CB_ERR_INVALID_ARG recorded.  Queries
  * are finite.
@@ -564,6 +567,8 @@ cb_status cb_block_select(cb_ctx* ctx, const cb_block_select_args* args, void* s
  *                       the chunk's own tokens up to its own
  *   cb_block_tree_attn  cb_tree_attn in which the cached context is that of the kv head's blocks; masks of any form (a row that sees no token and no
  *                       node is zero, its lse too)
+ * max_chunk decides between two kernels here too: with max_chunk * Hq / Hkv <= 16 a call of single tokens takes 17 to 50% less time than as a call of chunks, which
+ * it is taken for without that bound.
  * Arguments, outputs, errors and alignment are those of the dense calls (max_ctx bounds what it bounds there: a chunk's cached and new tokens, a tree's
  * cached ones).  A tree whose n_nodes is not in 0 .. T or whose ctx_len is negative (CB_ERR_INVALID_ARG recorded), or whose ctx_len exceeds max_ctx or
  * max_pages * P (CB_ERR_KV_FULL), gets zeros as if it had no nodes; without nodes its ctx_len is not looked at.  blocks int32 [batch, Hkv,

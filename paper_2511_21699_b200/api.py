@@ -377,7 +377,8 @@ class Cacheback:
                         max_ctx=0, blocks=None, stream=None):
         """The n_select blocks of its ctx_len[b] cached tokens that each sequence's queries score highest, per kv head, by rising number: blocks
         [batch, n_kv_heads, n_select], -1 behind the last.  The queries are a chunk's (q [rows, heads, head_dim] and q_start) or a tree's (q [batch, max_nodes,
-        heads, head_dim] and n_nodes).  The n_first first and the n_last newest blocks are always among them."""
+        heads, head_dim] and n_nodes).  The n_first first and the n_last newest blocks are always among them.  max_chunk, max_ctx: host upper bounds on a chunk's rows and
+        on every ctx_len (0: not known).  Give max_chunk=1 with single tokens: without it they are taken for chunks of all rows (64 sequences: three times as long)."""
         if blocks is None:
             blocks = _made(lambda: torch.empty(self.cfg.batch, self.cfg.n_kv_heads, n_select, dtype=torch.int32, device=self.device), stream, self.device)
         self._host.block_select(self._h, self._shape, q, k_mean, k_scale, block_table, ctx_len, q_start, n_nodes, block, n_select, n_first, n_last, max_chunk,
@@ -386,7 +387,8 @@ class Cacheback:
 
     def cb_block_attn(self, q, k_pool, v_pool, block_table, q_start, ctx_len, blocks, block=64, out=None, lse=None, max_chunk=0, max_ctx=0, scale=0.0,
                       stream=None):
-        """cb_chunk_attn over the selected blocks of the cached tokens and the chunk's own ones.  blocks: of cb_block_select, for the same ctx_len."""
+        """cb_chunk_attn over the selected blocks of the cached tokens and the chunk's own ones.  blocks: of cb_block_select, for the same ctx_len.  Give max_chunk=1 with
+        single tokens: without it they are taken for chunks of all rows."""
         if out is None:
             out = _made(lambda: torch.empty_like(q), stream, self.device)
         self._host.block_attn(self._h, self._shape, q, k_pool, v_pool, block_table, q_start, ctx_len, out, lse, max_chunk, max_ctx, scale, blocks, block,

@@ -1,6 +1,6 @@
 // Launchers of attention over selected blocks on the tensor cores: chunk attention's kernel (cb_chunk_tc.cuh), whose copies find their pages through the
 // lists, and whose rows may be a tree's nodes.  Measured with lists of 2,048 tokens, 64 query heads over 8 of 128: 8 chunks of 129 to 256 tokens 120 us in short runs, 142 in long
-// ones (the dense call over as many keys takes the same); 16 trees of 64 nodes 84 and 99 (the dense tree call 75 in short runs; 98 and 116 bytes of spills a thread here, 132 and 148 there).
+// ones (the dense call over as many keys takes the same); 16 trees of 64 nodes 84 and 99 (the dense tree call 75 in short runs; 94 and 112 bytes of spills a thread here, 132 and 148 there).
 #include <algorithm>
 
 #include "cb_chunk_tc.cuh"

@@ -1,7 +1,8 @@
 // Block summaries and the selection of blocks by them.
 //
-// cb_block_summary.  The mean of a block's keys, in 64 bits: a sum of up to 128 bf16 values is exact there (8-bit mantissas, unless exponents lie more than
-// 2^38 apart), so a block's tokens may be dealt to warps, a block may be summarised token by token or all at once, and the bits are the same.  A CTA takes
+// cb_block_summary.  The mean of a block's keys, in 64 bits: a sum of up to 128 bf16 values is exact there (8-bit mantissas) while their exponents lie no more than 38 apart, and
+// beyond that its bits follow from the order, which is always the same (a warp takes every eighth token, the warps are added up in turn).  So a block may be summarised token by
+// token or all at once, and the bits are the same.  A CTA takes
 // a block and 256 channels (two heads of 128 or four of 64): its eight warps take every eighth token, 512 contiguous bytes of it each, all of a warp's
 // loads under way at once, the next block's while this one's sums are put together in shared memory, where a thread finishes a channel.  Issue slots bound it, 64% of
 // them busy: 26.5 us for 100 MB of keys (8 heads of 128, blocks of 64), 3.8 TB/s; the block of one new token in each of 64 sequences 8 us from a cold start.
@@ -162,7 +163,8 @@ __global__ void __launch_bounds__(kSumThreads, S == 128 ? 2 : 3) cb_block_summar
 
 // ------------------------------------------------------------------------------------------------ selection by few queries
 // A warp takes 16 blocks at a time and has three such steps under way.  Four CTAs an SM, so that 592 units are resident at once (with 32 blocks in two steps, three
-// CTAs an SM, 68 of 512 units came in a second wave).
+// CTAs an SM, 68 of 512 units came in a second wave).  That many fit while the keys of all blocks that max_ctx allows take what the rings leave: up to 1,260 blocks
+// with 128 dims and 7,404 with 64; three up to 6,124 and 12,268.
 constexpr int kFewThreads = 256, kFewRows = 16, kFewStages = 3, kFewStep = kFewThreads / 32 * kFewRows;
 template <int D> constexpr int kFewWarpBytes = kFewStages * kFewRows * (D + 4);   // summaries and scales
 
@@ -172,7 +174,7 @@ __device__ __forceinline__ void mma_s8(int* c, uint32_t a0, uint32_t a1, uint32_
 }
 
 // Up to NT x 8 queries, single tokens mostly: memory's round trips are what a launch takes, so all that can be asked for at once is.  A warp's queries are its
-// own (a row of 8 lies in the registers of 32 lanes as the products take it), its 32 blocks' summaries come by asynchronous copies.
+// own (a row of 8 lies in the registers of 32 lanes as the products take it), its 16 blocks' summaries come by asynchronous copies.
 //
 // The products are m16n8k32 of bytes, 16 blocks by 8 queries by 32 dims (tcgen05's smallest tile of 128 blocks would wait for four warps' copies, for no gain: the
 // pipe is 2% busy).  A dot product does not mind the order of its terms, so the k-th step takes, of the 16-byte pieces that lane t of a row's four lanes holds
@@ -378,8 +380,12 @@ extern "C" cb_status cb_block_select(cb_ctx* ctx, const cb_block_select_args* a,
     const uint32_t over = p.g_inv * (uint32_t)p.G;            // G g_inv - 2^32, less than G
     if (over) p.max_chunk = std::min(p.max_chunk, (int)std::min<uint32_t>(0xFFFFFFFFu / over / (uint32_t)p.G, INT32_MAX));
     if (!p.q_start && (long long)p.B * p.T > 0x7FFFFFFFll) return CB_ERR_UNSUPPORTED;
-    // Up to 16 queries (rows x heads of the group) lie in a warp's registers; more are a matter of the tensor pipe, and of 128 blocks a tile.  With few units a
-    // cluster shares each one's blocks: as many CTAs as there are SMs for and tiles to keep them busy.
+    // Up to 16 queries (rows x heads of the group) lie in a warp's registers, the others are for the tensor pipe, and 128 blocks a tile.  (8 kv heads of 128; 64 sequences of 1 k to
+    // 32 k tokens in blocks of 64: 8 queries 10.0 and 33.5 us, 16 12.1 and 33.8; one of 32 k: 4.4 and 8.8, 5.2 and 8.8.  There are no forms for more queries than that; trial ones
+    // for 24 and 32 took 14.1 and 17.3 us against 33.9, and 5.6 and 6.4 against 8.9.)  With few units a
+    // cluster shares each one's blocks: as many CTAs as there are SMs for and tiles to keep them busy.  (Single tokens, 8 kv heads, 1, 2, 4 and 8 CTAs a unit: one
+    // sequence of 8 k tokens 4.0, 4.3, 4.2, 4.4 us, of 32 k 6.0, 5.3, 4.8, 4.8, of 128 k 17.5, 13.6, 11.6, 10.5; eight of 128 k 18.5, 14.4, 15.5, 17.9; 18 of 32 k 6.4, 6.6, 8.8, 13.4.
+    // Parts of 32 rows, where a CTA fills an SM: eight of 32 k 10.7, 10.2, 19.0, 41; twelve 10.8, 19.5, 27.8, 57.)
     const long long votes = (long long)(a->q_start ? p.max_chunk : p.T) * p.G;
     const int nt = votes <= 8 ? 1 : (votes <= 16 ? 2 : 0);
     int ctas = 1;

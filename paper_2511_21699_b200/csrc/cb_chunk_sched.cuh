@@ -65,7 +65,8 @@ struct CbChunkCuts {
 
 // TREE: the rows are the nodes of a draft tree, whose keys are a tile of their own behind the context's, the same for all rows.  The order is then that of tree attention,
 // (row group, sequence, kv head): all row groups read the same keys, and in this order do so at the same time, by CTAs a fixed part of the grid apart.  (16 trees
-// of 64 nodes, 64/8 heads over lists of 2,048 tokens: 306 MB from memory and 88 us with a sequence's row groups 8 units apart, 154 MB in this order.)
+// of 64 nodes, 64/8 heads over lists of 2,048 tokens: 306 MB from memory and 88 us with a sequence's row groups 8 units apart, 180 MB
+// and 84 us in this order; once each they are 153.  Chunks keep theirs: eight chunks of 129 to 256 tokens over such lists read 150 MB for 98, and wait for their softmax chains.)
 template <bool TREE>
 struct CbChunkShapeT {
     int row0 = 0, n = 0, ctx = 0, error = 0;
